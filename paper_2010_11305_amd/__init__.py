@@ -6,4 +6,4 @@ The compute path lives in HIP kernels behind the C ABI declared in
 package loads nothing; the binding loads the library on first use and raises if
 it has not been built.
 """
-__all__ = ["configs", "workload", "emb_cache"]
+__all__ = ["configs", "workload", "emb_cache", "mx4", "adamw"]

@@ -1,0 +1,121 @@
+"""AdamW over many tensors in one step, with moments in FP32 or in 8 bits (include/emb_dense.h).
+
+    opt = adamw.AdamW(params, lr=1e-3, state_bits=8, rounding="stochastic")
+    opt.step(grads)            # or opt.step(grads, lr=..., grad_scale=clip_factor)
+
+Parameters are updated in place.  The update runs in one HIP kernel per 192 tensors.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import dense_lib as lib
+
+
+class AdamW:
+    """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous.
+    weight_decay: one number, or one per tensor.  grad_dtype: the type of the gradients (default:
+    that of the parameters)."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_dtype=None,
+                 state_bits=32, rounding="nearest", seed=0):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("params must hold at least one tensor")
+        p0 = self.params[0]
+        self.dtype, self.device = p0.dtype, p0.device
+        self.grad_dtype = grad_dtype or self.dtype
+        for p in self.params:
+            if p.dtype != self.dtype or p.device != self.device or not p.is_cuda or not p.is_contiguous():
+                raise ValueError("params must be contiguous tensors of one type on one GPU")
+        n = len(self.params)
+        self.sizes = [p.numel() for p in self.params]
+        self.lr, self.state_bits = float(lr), state_bits
+        c = lib.AdamwConfig()
+        self._sizes = (ctypes.c_int64 * n)(*self.sizes)
+        c.num_tensors, c.param_type, c.sizes = n, lib.type_of(self.dtype), self._sizes
+        if isinstance(weight_decay, (int, float)):
+            c.weight_decay = float(weight_decay)
+        else:
+            weight_decay = [float(w) for w in weight_decay]
+            if len(weight_decay) != n:
+                raise ValueError("weight_decay must be a number, or one for each tensor")
+            self._decays = (ctypes.c_double * n)(*weight_decay)
+            c.weight_decays = self._decays
+        c.grad_type, c.state_bits, c.rounding = lib.type_of(self.grad_dtype), int(state_bits), lib.rounding_of(rounding)
+        c.beta1, c.beta2, c.eps, c.seed = float(betas[0]), float(betas[1]), float(eps), int(seed)
+        L = lib.load()
+        self._layout = lib.AdamwSizes()
+        lib.check(L.emb_adamw_query_sizes(ctypes.byref(c), ctypes.byref(self._layout)), "emb_adamw_query_sizes")
+        self.state_buffer = torch.empty(max(self._layout.state_bytes, 256), dtype=torch.uint8, device=self.device)
+        self._h = ctypes.c_void_p()
+        with lib.on_device(self.device):
+            lib.check(L.emb_adamw_create(ctypes.byref(c), self.state_buffer.data_ptr(), self._layout.state_bytes,
+                                         lib.stream(self.device), ctypes.byref(self._h)), "emb_adamw_create")
+        self._pointers = ctypes.c_void_p * n
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib.load().emb_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, grads, lr=None, grad_scale=None):
+        """One step.  grads: one tensor per parameter, contiguous, of grad_dtype; None leaves the parameter and
+        its moments as they are.  grad_scale: a float32 scalar tensor on the GPU that multiplies them."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
+        gp, gd, dev = [], self.grad_dtype, self.device
+        for g, n in zip(grads, self.sizes):
+            if g is None:
+                gp.append(None)
+                continue
+            if g.dtype != gd or g.numel() != n or g.device != dev or not g.is_contiguous():
+                raise ValueError(f"a gradient must be contiguous, {gd}, on {dev}, and as large as its parameter")
+            gp.append(g.data_ptr())
+        scale = None
+        if grad_scale is not None:
+            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
+                raise ValueError(f"grad_scale must be one float32 value on {dev}")
+            scale = grad_scale.data_ptr()
+        with lib.on_device(dev):
+            lib.check(lib.load().emb_adamw_step(self._h, self._pointers(*[p.data_ptr() for p in self.params]),
+                                                self._pointers(*gp), self.lr if lr is None else float(lr), scale,
+                                                lib.stream(dev)), "emb_adamw_step")
+
+    def state(self) -> dict:
+        """The moments, as views of the state buffer over all tensors, each tensor's part padded to a multiple of 32
+        elements: exp_avg and exp_avg_sq (32 bits), or exp_avg and exp_avg_root (E4M3 elements) with the scale
+        byte of each 32 in exp_avg_scale and exp_avg_root_scale."""
+        s, n = self._layout, self._layout.elements
+
+        def view(offset, count, dtype):
+            size = torch.empty((), dtype=dtype).element_size()
+            return self.state_buffer[offset:offset + count * size].view(dtype)
+
+        if self.state_bits == 32:
+            return {"exp_avg": view(s.first_offset, n, torch.float32),
+                    "exp_avg_sq": view(s.second_offset, n, torch.float32)}
+        return {"exp_avg": view(s.first_offset, n, torch.float8_e4m3fn),
+                "exp_avg_root": view(s.second_offset, n, torch.float8_e4m3fn),
+                "exp_avg_scale": view(s.first_scale_offset, n // 32, torch.uint8),
+                "exp_avg_root_scale": view(s.second_scale_offset, n // 32, torch.uint8)}
+
+    @property
+    def step_count(self) -> int:
+        """Steps done."""
+        v = ctypes.c_uint64()
+        lib.check(lib.load().emb_adamw_get_step(self._h, ctypes.byref(v)), "emb_adamw_get_step")
+        return int(v.value)
+
+    @step_count.setter
+    def step_count(self, steps: int):
+        lib.check(lib.load().emb_adamw_set_step(self._h, int(steps)), "emb_adamw_set_step")

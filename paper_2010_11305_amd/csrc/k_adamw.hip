@@ -1,0 +1,238 @@
+// One AdamW step over many tensors.
+//
+// Every element is read and written once; the bound is the copy rate.  A workgroup takes one
+// part (up to kAdamChunk elements) of one tensor, found in a table that was laid out with
+// the state, so that tensors of any number and size are one launch per kAdamTensors of
+// them and no workgroup searches.  The pointers travel in the kernel arguments: they may
+// change from step to step without a copy to the device.  A thread holds 8 consecutive
+// elements, so a block of 32 that shares a scale is 4 neighbouring lanes.
+#include "dense_device.h"
+
+namespace embd {
+
+namespace {
+
+constexpr int kPer = 8;
+
+// The largest of a value over the 4 lanes of a quad.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, false));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, false));
+}
+
+// Scale byte of a block of E4M3 elements: the smallest power of two with which its largest
+// magnitude is at most 448 = 1.75 * 2^8.
+__device__ __forceinline__ uint32_t e4m3_scale(uint32_t amax) {
+  const int e = (int)(amax >> 23);
+  if (e == 255) return 255u;
+  const int s = e - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return s < 0 ? 0u : (uint32_t)s;
+}
+
+// |x| / 2^s <= 448 to a multiple of its step, as an FP32 value that E4M3 holds exactly.
+// u: 16 random bits, unused when rounding to nearest.
+template <bool STOCHASTIC, bool KEEP>
+__device__ __forceinline__ float e4m3_round(float x, float inv, uint32_t u) {
+  const float y = fabsf(x) * inv;
+  int e = (int)(__float_as_uint(y) >> 23) - 127;
+  e = e < -6 ? -6 : e;
+  const float t = ldexpf(y, 3 - e);
+  float k;
+  if constexpr (STOCHASTIC) {
+    k = floorf(t);
+    k += (float)u * 0x1p-16f < t - k ? 1.0f : 0.0f;
+  } else {
+    k = rintf(t);
+  }
+  if constexpr (KEEP) k = k < 1.0f && x > 0.0f ? 1.0f : k;
+  return copysignf(ldexpf(k, e - 3), x);
+}
+
+// 8 moments of a lane to 8 E4M3 elements and the scale byte of the quad's block.
+template <bool STOCHASTIC, bool KEEP>
+__device__ __forceinline__ uint2 e4m3_pack(const float (&x)[kPer], const uint32_t (&u)[kPer], uint32_t* scale) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) a = max(a, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+  const uint32_t s = e4m3_scale(quad_max(a));
+  *scale = s;
+  if (s == 255u) return make_uint2(0, 0);
+  const float inv = power_of(254u - s);
+  float q[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) q[j] = e4m3_round<STOCHASTIC, KEEP>(x[j], inv, u[j]);
+  int w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
+    w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w[i], true);
+  }
+  return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+}
+
+__device__ __forceinline__ void e4m3_unpack(uint2 w, uint32_t scale, float (&x)[kPer]) {
+  const float f = scale == 255u ? __uint_as_float(0x7FC00000u) : power_of(scale);
+  const uint32_t ws[2] = {w.x, w.y};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)ws[i], false);
+    const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)ws[i], true);
+    x[4 * i] = lo[0] * f, x[4 * i + 1] = lo[1] * f, x[4 * i + 2] = hi[0] * f, x[4 * i + 3] = hi[1] * f;
+  }
+}
+
+template <int PT, int GT, int BITS, bool STOCHASTIC>
+__global__ __launch_bounds__(256) void k_adamw(AdamDev d, AdamPointers ptr, uint32_t first, int64_t part0, AdamConst c,
+                                               const float* __restrict__ grad_scale) {
+  const AdamPart part = d.parts[part0 + blockIdx.x];
+  const uint32_t slot = part.tensor - first;
+  using P = typename Elem<PT>::type;
+  using G = typename Elem<GT>::type;
+  P* p = static_cast<P*>(ptr.p[slot]);
+  const G* g = static_cast<const G*>(ptr.g[slot]);
+  if (!g) return;
+  const AdamTensor t = d.tensors[part.tensor];
+  const float keep = (float)(1.0 - c.lr * t.decay);
+  const float gs = grad_scale ? *grad_scale : 1.0f;
+#pragma unroll
+  for (int it = 0; it < kAdamChunk / (256 * kPer); ++it) {
+    const int64_t i = (int64_t)part.chunk * kAdamChunk + (it * 256 + threadIdx.x) * kPer;
+    // a block of 32 that the tensor reaches into is worked on by its whole quad
+    if (i >= (t.size + kBlock - 1) / kBlock * kBlock) return;
+    const int n = t.size - i >= kPer ? kPer : t.size > i ? (int)(t.size - i) : 0;
+    Raw<PT, kPer> rp;
+    Raw<GT, kPer> rg;
+    load_values(p + (n ? i : 0), n, rp);
+    load_values(g + (n ? i : 0), n, rg);
+    const int64_t at = t.base + i;
+    float m[kPer], v[kPer];
+    if constexpr (BITS == 32) {
+      const float4* sm = reinterpret_cast<const float4*>(d.first) + at / 4;
+      const float4* sv = reinterpret_cast<const float4*>(d.second) + at / 4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 a = sm[h], b = sv[h];
+        m[4 * h] = a.x, m[4 * h + 1] = a.y, m[4 * h + 2] = a.z, m[4 * h + 3] = a.w;
+        v[4 * h] = b.x, v[4 * h + 1] = b.y, v[4 * h + 2] = b.z, v[4 * h + 3] = b.w;
+      }
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(d.first + at), b = *reinterpret_cast<const uint2*>(d.second + at);
+      e4m3_unpack(a, d.first_scale[at / kBlock], m);
+      e4m3_unpack(b, d.second_scale[at / kBlock], v);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) v[j] = v[j] * v[j];
+    }
+    uint32_t word[kPer] = {};
+    if constexpr (STOCHASTIC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint64_t n4 = (uint64_t)(at / 4 + h);
+        const uint4 w = embc::philox4x32_10(make_uint4((uint32_t)n4, (uint32_t)(n4 >> 32), c.t, 0), c.k0, c.k1);
+        word[4 * h] = w.x, word[4 * h + 1] = w.y, word[4 * h + 2] = w.z, word[4 * h + 3] = w.w;
+      }
+    }
+    float root[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const float gj = rg.get(j) * gs;
+      m[j] = m[j] * c.beta1 + gj * c.rest1;
+      v[j] = v[j] * c.beta2 + (gj * gj) * c.rest2;
+      root[j] = __fsqrt_rn(v[j]);
+      const float away = m[j] / (root[j] * c.inv_root + c.eps);
+      const float x = rp.get(j) * keep - away * c.rate;
+      if constexpr (PT == EMB_TYPE_FP32) {
+        rp.w[j] = __float_as_uint(x);
+      } else if constexpr (STOCHASTIC) {
+        const uint32_t b = __float_as_uint(x), u = (word[j] ^ word[j] >> 16) & 0xFFFFu;
+        const bool whole = (b & 0x7F800000u) == 0x7F800000u;  // infinities and NaN are kept
+        rp.put(j, whole ? bf16_bits(x) : (b + u) >> 16);
+      } else {
+        rp.put(j, bf16_bits(x));
+      }
+    }
+    if (n < kPer) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (j >= n) m[j] = 0.0f, v[j] = 0.0f, root[j] = 0.0f;
+    }
+    if (n == kPer) {
+#pragma unroll
+      for (int h = 0; h < Raw<PT, kPer>::kWords / 4; ++h) {
+        const Bytes16 b = {{rp.w[4 * h], rp.w[4 * h + 1], rp.w[4 * h + 2], rp.w[4 * h + 3]}};
+        reinterpret_cast<Bytes16*>(p + i)[h] = b;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        if (j >= n) continue;
+        if constexpr (PT == EMB_TYPE_FP32)
+          p[i + j] = __uint_as_float(rp.w[j]);
+        else
+          p[i + j] = (uint16_t)(j % 2 ? rp.w[j / 2] >> 16 : rp.w[j / 2]);
+      }
+    }
+    if constexpr (BITS == 32) {
+      float4* sm = reinterpret_cast<float4*>(d.first) + at / 4;
+      float4* sv = reinterpret_cast<float4*>(d.second) + at / 4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sm[h] = make_float4(m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]);
+        sv[h] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+      }
+    } else {
+      uint32_t um[kPer], ur[kPer], s1, s2;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) um[j] = word[j] & 0xFFFFu, ur[j] = word[j] >> 16;
+      const uint2 a = e4m3_pack<STOCHASTIC, false>(m, um, &s1);
+      const uint2 b = e4m3_pack<STOCHASTIC, true>(root, ur, &s2);
+      *reinterpret_cast<uint2*>(d.first + at) = a;
+      *reinterpret_cast<uint2*>(d.second + at) = b;
+      if (threadIdx.x % 4 == 0) {
+        d.first_scale[at / kBlock] = (uint8_t)s1;
+        d.second_scale[at / kBlock] = (uint8_t)s2;
+      }
+    }
+  }
+}
+
+template <int PT, int GT>
+hipError_t adamw_as(const AdamDev& d, const AdamPointers& ptr, uint32_t first, int64_t part0, int64_t parts,
+                    const AdamConst& c, const float* gs, int bits, int rounding, hipStream_t s) {
+  const unsigned grid = (unsigned)parts;
+  const bool random = rounding == EMB_ROUND_STOCHASTIC && (bits == 8 || PT != EMB_TYPE_FP32);
+  if (bits == 32) {
+    if constexpr (PT != EMB_TYPE_FP32) {
+      if (random) {
+        k_adamw<PT, GT, 32, true><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+        return hipGetLastError();
+      }
+    }
+    k_adamw<PT, GT, 32, false><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+  } else if (random) {
+    k_adamw<PT, GT, 8, true><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+  } else {
+    k_adamw<PT, GT, 8, false><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamDev& d, const AdamPointers& ptr, uint32_t first, int64_t part0, int64_t parts,
+                        const AdamConst& c, const float* grad_scale, int param_type, int grad_type, int state_bits,
+                        int rounding, hipStream_t s) {
+#define EMBD_GRAD(PT)                                                                                         \
+  switch (grad_type) {                                                                                        \
+    case EMB_TYPE_FP32:                                                                                       \
+      return adamw_as<PT, EMB_TYPE_FP32>(d, ptr, first, part0, parts, c, grad_scale, state_bits, rounding, s); \
+    case EMB_TYPE_BF16:                                                                                       \
+      return adamw_as<PT, EMB_TYPE_BF16>(d, ptr, first, part0, parts, c, grad_scale, state_bits, rounding, s); \
+    default:                                                                                                  \
+      return adamw_as<PT, EMB_TYPE_FP16>(d, ptr, first, part0, parts, c, grad_scale, state_bits, rounding, s); \
+  }
+  if (param_type == EMB_TYPE_FP32) EMBD_GRAD(EMB_TYPE_FP32)
+  EMBD_GRAD(EMB_TYPE_BF16)
+#undef EMBD_GRAD
+}
+
+}  // namespace embd

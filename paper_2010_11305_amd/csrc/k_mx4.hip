@@ -1,0 +1,242 @@
+// MX4 matrices: quantisation by rows and by columns, expansion, and the plain codes.
+//
+// Every kernel moves bytes and does little else: the bound is the copy rate.
+#include "dense_device.h"
+
+namespace embd {
+
+namespace {
+
+// By rows: a wave takes one tile, lane 16 b + r quantises block b of row r by itself (no
+// step crosses lanes), and the wave writes the tile's 1024 bytes as they lie.
+template <int TYPE, bool STOCHASTIC>
+__global__ __launch_bounds__(256) void k_quantize_rows(const typename Elem<TYPE>::type* __restrict__ x, Mx4 q,
+                                                       int64_t ld, uint8_t* __restrict__ out, Mx4Random rnd) {
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= q.row_tiles * q.col_tiles) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
+  const int64_t left = row < q.rows ? q.cols - col : 0;
+  Raw<TYPE, kBlock> r;
+  load_values(x + (left > 0 ? row * ld + col : 0), (int)(left < 0 ? 0 : left > kBlock ? kBlock : left), r);
+  uint32_t s;
+  const uint4 c = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
+  *reinterpret_cast<uint4*>(out + q.tile(rt, kt) + 16 * lane) = c;
+  out[q.scale(rt, kt, lane)] = (uint8_t)s;
+}
+
+// By columns, and by rows from the same pass: a workgroup stages 128 rows x 64 columns in
+// LDS; then a thread takes 32 rows of one column (a wave: 64 columns, so its reads of a
+// row are contiguous), and, for the rows, 32 columns of one row.
+constexpr int kStageRows = 128, kStageCols = 64;
+
+template <int TYPE, bool STOCHASTIC, bool ROWS>
+__global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TYPE>::type* __restrict__ x, Mx4 qr,
+                                                          Mx4 qc, int64_t ld, uint8_t* __restrict__ by_rows,
+                                                          uint8_t* __restrict__ by_columns, Mx4Random rnd) {
+  using E = typename Elem<TYPE>::type;
+  constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
+  constexpr int kPitch = kStageCols + kPiece;  // 16 more bytes a row: rows start in different banks
+  __shared__ __attribute__((aligned(16))) E stage[kStageRows * kPitch];
+  const int64_t tiles_c = (qr.cols + kStageCols - 1) / kStageCols;
+  const int64_t row0 = (int64_t)blockIdx.x / tiles_c * kStageRows, col0 = (int64_t)blockIdx.x % tiles_c * kStageCols;
+  constexpr int kPieces = kStageCols / kPiece;
+#pragma unroll
+  for (int i = 0; i < kStageRows * kPieces / 256; ++i) {
+    const int id = i * 256 + threadIdx.x, r = id / kPieces, c = id % kPieces * kPiece;
+    const int64_t row = row0 + r, left = row < qr.rows ? qr.cols - col0 - c : 0;
+    Raw<TYPE, kPiece> v;
+    load_values(x + (left > 0 ? row * ld + col0 + c : 0), (int)(left < 0 ? 0 : left > kPiece ? kPiece : left), v);
+    *reinterpret_cast<uint4*>(&stage[r * kPitch + c]) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  }
+  __syncthreads();
+  {
+    const int c = threadIdx.x & 63, b = threadIdx.x >> 6;
+    const int64_t col = col0 + c, rt = col / kTileRows, kt = row0 / kTileCols;
+    if (rt < qc.row_tiles) {
+      Raw<TYPE, kBlock> r;
+#pragma unroll
+      for (int j = 0; j < kBlock; ++j) r.put(j, load_bits<TYPE>(&stage[(b * kBlock + j) * kPitch + c]));
+      uint32_t s;
+      Mx4Random q = rnd;
+      q.tag = 1;
+      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)((row0 + b * kBlock) / 8), (uint32_t)col, q, &s);
+      const int lane = b * 16 + (int)(col % kTileRows);
+      *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
+      by_columns[qc.scale(rt, kt, lane)] = (uint8_t)s;
+    }
+  }
+  if constexpr (ROWS) {
+    const int rr = threadIdx.x & 127, h = threadIdx.x >> 7;
+    const int64_t row = row0 + rr, rt = row / kTileRows, kt = col0 / kTileCols;
+    if (rt < qr.row_tiles) {
+      Raw<TYPE, kBlock> r;
+#pragma unroll
+      for (int i = 0; i < kBlock / kPiece; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(&stage[rr * kPitch + h * kBlock + i * kPiece]);
+        r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
+      }
+      uint32_t s;
+      const int64_t col = col0 + h * kBlock;
+      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
+      const int lane = (int)(col % kTileCols / kBlock) * 16 + (int)(row % kTileRows);
+      *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * lane) = code;
+      by_rows[qr.scale(rt, kt, lane)] = (uint8_t)s;
+      // the tile's other half, where no column of x is left for a workgroup of its own
+      if (col0 + kStageCols >= qr.cols && col0 % kTileCols == 0) {
+        *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * (lane + 32)) = make_uint4(0, 0, 0, 0);
+        by_rows[qr.scale(rt, kt, lane + 32)] = 0;
+      }
+    }
+  }
+}
+
+// Expansion: a thread takes 8 values (one dword of codes), 16 consecutive threads one row of a
+// tile, so that a wave writes whole lines.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::type* __restrict__ x, int64_t ld) {
+  const int64_t tile = blockIdx.x;
+  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int rr = threadIdx.x >> 4, c8 = threadIdx.x & 15, lane = (c8 >> 2) * 16 + rr;
+  const int64_t row = rt * kTileRows + rr, col = kt * kTileCols + c8 * 8;
+  if (row >= q.rows || col >= q.cols) return;
+  const uint32_t c = *reinterpret_cast<const uint32_t*>(q.base + q.tile(rt, kt) + 16 * lane + 4 * (c8 & 3));
+  const uint32_t s = q.base[q.scale(rt, kt, lane)];
+  Raw<TYPE, 8> r;
+#pragma unroll
+  for (int j = 0; j < Raw<TYPE, 8>::kWords; ++j) r.w[j] = 0;
+  const float f = power_of(s);
+  f32x2 v[4];
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 0);
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 1);
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 2);
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, f, 3);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.put(j, to_bits<TYPE>(s == 255u ? __uint_as_float(0x7FC00000u) : v[j / 2][j % 2]));
+  typename Elem<TYPE>::type* p = x + row * ld + col;
+  const int n = q.cols - col < 8 ? (int)(q.cols - col) : 8;
+  if (n == 8) {
+#pragma unroll
+    for (int i = 0; i < Raw<TYPE, 8>::kWords / 4; ++i) {
+      Bytes16 b = {{r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]}};
+      reinterpret_cast<Bytes16*>(p)[i] = b;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= n) continue;
+      if constexpr (TYPE == EMB_TYPE_FP32)
+        p[j] = __uint_as_float(r.w[j]);
+      else
+        p[j] = (uint16_t)(j % 2 ? r.w[j / 2] >> 16 : r.w[j / 2]);
+    }
+  }
+}
+
+// Plain codes to tiles and back: a thread takes one block.
+__global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                              Mx4 q, uint8_t* __restrict__ out) {
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= q.row_tiles * q.col_tiles) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
+  const int64_t left = row < q.rows ? q.cols - col : 0;
+  const int n = (int)(left < 0 ? 0 : left > kBlock ? kBlock : left);
+  const int64_t pitch = (q.cols + 1) / 2, blocks = (q.cols + kBlock - 1) / kBlock;
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kBlock / 2; ++i) {
+    if (2 * i >= n) continue;
+    uint32_t b = codes[row * pitch + col / 2 + i];
+    if (2 * i + 1 >= n) b &= 15u;
+    w[i / 4] |= b << (8 * (i % 4));
+  }
+  *reinterpret_cast<uint4*>(out + q.tile(rt, kt) + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+  out[q.scale(rt, kt, lane)] = n > 0 ? scales[row * blocks + col / kBlock] : (uint8_t)0;
+}
+
+__global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= q.row_tiles * q.col_tiles) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
+  const int64_t left = row < q.rows ? q.cols - col : 0;
+  if (left <= 0) return;
+  const int n = (int)(left > kBlock ? kBlock : left);
+  const int64_t pitch = (q.cols + 1) / 2, blocks = (q.cols + kBlock - 1) / kBlock;
+  const uint4 v = *reinterpret_cast<const uint4*>(q.base + q.tile(rt, kt) + 16 * lane);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < kBlock / 2; ++i)
+    if (2 * i < n) codes[row * pitch + col / 2 + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  scales[row * blocks + col / kBlock] = q.base[q.scale(rt, kt, lane)];
+}
+
+template <int TYPE, bool STOCHASTIC>
+hipError_t quantize_as(const void* xv, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
+                       const Mx4Random& rnd, hipStream_t s) {
+  const auto* x = static_cast<const typename Elem<TYPE>::type*>(xv);
+  const Mx4 qr(by_rows, rows, cols), qc(by_columns, cols, rows);
+  auto* r = static_cast<uint8_t*>(by_rows);
+  auto* c = static_cast<uint8_t*>(by_columns);
+  if (!c) {
+    const int64_t tiles = qr.row_tiles * qr.col_tiles;
+    k_quantize_rows<TYPE, STOCHASTIC><<<(unsigned)((tiles + 3) / 4), 256, 0, s>>>(x, qr, ld, r, rnd);
+  } else {
+    const unsigned grid = (unsigned)(((rows + kStageRows - 1) / kStageRows) * ((cols + kStageCols - 1) / kStageCols));
+    if (r)
+      k_quantize_columns<TYPE, STOCHASTIC, true><<<grid, 256, 0, s>>>(x, qr, qc, ld, r, c, rnd);
+    else
+      k_quantize_columns<TYPE, STOCHASTIC, false><<<grid, 256, 0, s>>>(x, qr, qc, ld, r, c, rnd);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t ld, void* by_rows,
+                           void* by_columns, int rounding, uint64_t seed, uint32_t step, hipStream_t s) {
+  const Mx4Random rnd = {(uint32_t)seed, (uint32_t)(seed >> 32), step, 0};
+  const bool sr = rounding == EMB_ROUND_STOCHASTIC;
+  switch (type) {
+    case EMB_TYPE_FP32:
+      return sr ? quantize_as<EMB_TYPE_FP32, true>(x, rows, cols, ld, by_rows, by_columns, rnd, s)
+                : quantize_as<EMB_TYPE_FP32, false>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
+    case EMB_TYPE_BF16:
+      return sr ? quantize_as<EMB_TYPE_BF16, true>(x, rows, cols, ld, by_rows, by_columns, rnd, s)
+                : quantize_as<EMB_TYPE_BF16, false>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
+    default:
+      return sr ? quantize_as<EMB_TYPE_FP16, true>(x, rows, cols, ld, by_rows, by_columns, rnd, s)
+                : quantize_as<EMB_TYPE_FP16, false>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
+  }
+}
+
+hipError_t launch_dequantize(const void* qv, int64_t rows, int64_t cols, void* x, int type, int64_t ld, hipStream_t s) {
+  const Mx4 q(qv, rows, cols);
+  const unsigned grid = (unsigned)(q.row_tiles * q.col_tiles);
+  if (type == EMB_TYPE_FP32)
+    k_dequantize<EMB_TYPE_FP32><<<grid, 256, 0, s>>>(q, static_cast<float*>(x), ld);
+  else if (type == EMB_TYPE_BF16)
+    k_dequantize<EMB_TYPE_BF16><<<grid, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld);
+  else
+    k_dequantize<EMB_TYPE_FP16><<<grid, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld);
+  return hipGetLastError();
+}
+
+hipError_t launch_pack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* qv,
+                       hipStream_t s) {
+  const Mx4 q(qv, rows, cols);
+  k_pack<<<(unsigned)((q.row_tiles * q.col_tiles + 3) / 4), 256, 0, s>>>(codes, scales, q, static_cast<uint8_t*>(qv));
+  return hipGetLastError();
+}
+
+hipError_t launch_unpack(const void* qv, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const Mx4 q(qv, rows, cols);
+  k_unpack<<<(unsigned)((q.row_tiles * q.col_tiles + 3) / 4), 256, 0, s>>>(q, codes, scales);
+  return hipGetLastError();
+}
+
+}  // namespace embd

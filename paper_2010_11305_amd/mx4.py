@@ -1,0 +1,213 @@
+"""Matrices in microscaled 4-bit floating point and the linear layer on them (include/emb_dense.h).
+
+A block of 32 consecutive values of a row shares a power of two; each value is a 4-bit code
+(sign, 2 exponent bits, 1 mantissa bit).  The bindings only marshal arguments; every step
+runs in the HIP kernels of libembcache, on the current stream.
+
+    w4 = mx4.quantize(w)                   # [n, k]
+    y = mx4.linear(x, w4)                  # [m, n] = Q(x) w4^T, x in full precision
+    c = mx4.matmul(a4, b4, torch.float32)  # a4 b4^T
+
+    layer = mx4.Linear(n, k)               # training
+    layer.load(w)
+    y, saved = layer.forward_train(x)
+    dx, dw = layer.backward(dy, saved, step)
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import dense_lib as lib
+
+_bytes_of = {}
+
+
+def _query(name, *dims) -> int:
+    """Buffer sizes are functions of the dimensions alone."""
+    key = (name, dims)
+    n = _bytes_of.get(key)
+    if n is None:
+        v = ctypes.c_size_t()
+        lib.check(getattr(lib.load(), name)(*dims, ctypes.byref(v)), name)
+        if len(_bytes_of) > 4096:
+            _bytes_of.clear()
+        n = _bytes_of[key] = v.value
+    return n
+
+
+class Mx4Matrix:
+    """rows x cols values in 4 bits, in one device buffer (`data`, uint8)."""
+
+    __slots__ = ("rows", "cols", "data")
+
+    def __init__(self, rows: int, cols: int, device="cuda", data=None):
+        need = _query("emb_mx4_query_bytes", rows, cols)
+        if data is None:
+            data = torch.empty(need, dtype=torch.uint8, device=device)
+        elif data.dtype != torch.uint8 or not data.is_cuda or not data.is_contiguous() or data.numel() < need:
+            raise ValueError(f"data must be at least {need} contiguous bytes on the GPU")
+        self.rows, self.cols, self.data = rows, cols, data
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @property
+    def device(self):
+        return self.data.device
+
+    def dequantize(self, dtype=torch.float32, out=None):
+        """The values as a [rows, cols] tensor (exact in float32 and bfloat16)."""
+        if out is None:
+            out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.data.device)
+        p, t, rows, cols, ld = lib.matrix(out, "out")
+        if (rows, cols) != self.shape or out.device != self.device:
+            raise ValueError(f"out must be {self.shape} on {self.device}")
+        with lib.on_device(self.device):
+            lib.check(lib.load().emb_mx4_dequantize(self.data.data_ptr(), rows, cols, p, t, ld, lib.stream(self.device)),
+                      "emb_mx4_dequantize")
+        return out
+
+    def to_codes(self):
+        """(codes [rows, ceil(cols/2)], scales [rows, ceil(cols/32)]) as uint8 tensors, codes two a
+        byte with the even column in the low half: the plain form, for checkpoints and exchange."""
+        codes = torch.empty((self.rows, -(-self.cols // 2)), dtype=torch.uint8, device=self.device)
+        scales = torch.empty((self.rows, -(-self.cols // 32)), dtype=torch.uint8, device=self.device)
+        with lib.on_device(self.device):
+            lib.check(lib.load().emb_mx4_unpack(self.data.data_ptr(), self.rows, self.cols, codes.data_ptr(),
+                                                scales.data_ptr(), lib.stream(self.device)), "emb_mx4_unpack")
+        return codes, scales
+
+
+def from_codes(codes, scales, cols: int, out: Mx4Matrix | None = None) -> Mx4Matrix:
+    """The inverse of Mx4Matrix.to_codes."""
+    rows = codes.shape[0]
+    for t, width, what in ((codes, -(-cols // 2), "codes"), (scales, -(-cols // 32), "scales")):
+        if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != (rows, width):
+            raise ValueError(f"{what} must be a contiguous uint8 tensor [{rows}, {width}] on the GPU")
+    out = _target(out, rows, cols, codes.device, "out")
+    with lib.on_device(out.device):
+        lib.check(lib.load().emb_mx4_pack(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data.data_ptr(),
+                                          lib.stream(out.device)), "emb_mx4_pack")
+    return out
+
+
+def _target(out, rows, cols, device, what) -> Mx4Matrix:
+    if out is None:
+        return Mx4Matrix(rows, cols, device)
+    if out.shape != (rows, cols) or out.device != device:
+        raise ValueError(f"{what} must be an Mx4Matrix [{rows}, {cols}] on {device}")
+    return out
+
+
+def _quantize(x, rows_out, columns_out, rounding, seed, step):
+    """rows_out, columns_out: an Mx4Matrix to fill, None for a new one, False for none."""
+    p, t, rows, cols, ld = lib.matrix(x, "x")
+    by_rows = None if rows_out is False else _target(rows_out, rows, cols, x.device, "the matrix by rows")
+    by_columns = None if columns_out is False else _target(columns_out, cols, rows, x.device, "the matrix by columns")
+    with lib.on_device(x.device):
+        lib.check(lib.load().emb_mx4_quantize(p, t, rows, cols, ld, by_rows.data.data_ptr() if by_rows else None,
+                                              by_columns.data.data_ptr() if by_columns else None,
+                                              lib.rounding_of(rounding), seed, step, lib.stream(x.device)),
+                  "emb_mx4_quantize")
+    return by_rows, by_columns
+
+
+def quantize(x, rounding="nearest", seed=0, step=0, out: Mx4Matrix | None = None) -> Mx4Matrix:
+    """x [rows, cols] in 4 bits, blocks along its rows.  Stochastic rounding draws from (seed, step)."""
+    return _quantize(x, out, False, rounding, seed, step)[0]
+
+
+def quantize_columns(x, rounding="nearest", seed=0, step=0, out: Mx4Matrix | None = None) -> Mx4Matrix:
+    """The transpose of x in 4 bits, [cols, rows], blocks along the columns of x."""
+    return _quantize(x, False, out, rounding, seed, step)[1]
+
+
+def quantize_both(x, rounding="nearest", seed=0, step=0, out=(None, None)):
+    """(quantize(x), quantize_columns(x)) with x read once."""
+    return _quantize(x, out[0], out[1], rounding, seed, step)
+
+
+def _result(out, rows, cols, dtype, device):
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=device)
+    p, t, r, c, ld = lib.matrix(out, "out")
+    if (r, c) != (rows, cols) or out.device != device:
+        raise ValueError(f"out must be [{rows}, {cols}] on {device}")
+    return out, p, t, ld
+
+
+def _workspace(bytes_, device):
+    return torch.empty(bytes_, dtype=torch.uint8, device=device) if bytes_ else None
+
+
+def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
+    """a b^T for a [m, k] and b [n, k]: FP32 sums, one rounding to dtype (or to out's)."""
+    if a.cols != b.cols or a.device != b.device:
+        raise ValueError(f"a {a.shape} and b {b.shape} must have the same number of columns, on one device")
+    dev = a.device
+    out, p, t, ld = _result(out, a.rows, b.rows, dtype, dev)
+    need = _query("emb_mx4_matmul_workspace", a.rows, b.rows, a.cols)
+    ws = _workspace(need, dev)
+    with lib.on_device(dev):
+        lib.check(lib.load().emb_mx4_matmul(a.data.data_ptr(), b.data.data_ptr(), a.rows, b.rows, a.cols, p, t, ld,
+                                            ws.data_ptr() if need else None, need, lib.stream(dev)), "emb_mx4_matmul")
+    return out
+
+
+def linear(x, w: Mx4Matrix, out=None):
+    """Q(x) w^T for full-precision rows x [m, k] and a weight w [n, k] in 4 bits, in the type of x."""
+    p, t, m, k, ld = lib.matrix(x, "x")
+    dev = x.device
+    if k != w.cols or w.device != dev:
+        raise ValueError(f"x [{m}, {k}] and w {w.shape} must have the same number of columns, on one device")
+    out, yp, yt, yld = _result(out, m, w.rows, x.dtype, dev)
+    if yt != t:
+        raise ValueError("out must have the type of x")
+    need = _query("emb_mx4_linear_workspace", m, w.rows, k)
+    ws = _workspace(need, dev)
+    with lib.on_device(dev):
+        lib.check(lib.load().emb_mx4_linear(p, t, m, k, ld, w.data.data_ptr(), w.rows, yp, yld,
+                                            ws.data_ptr() if need else None, need, lib.stream(dev)), "emb_mx4_linear")
+    return out
+
+
+class Linear:
+    """The products of a linear layer y = x w^T in 4 bits, forward and backward.
+
+    The full-precision weight stays with the caller (and its optimizer); load() brings it
+    here in 4 bits along both axes, after every update.  Rows and weights round as
+    `rounding` says, output gradients as `grad_rounding` does: stochastic rounding keeps
+    gradients unbiased.
+
+        y  = Q(x) Q(w)^T
+        dx = Q(dy) Q(w^T)^T        blocks along the outputs
+        dw = Q(dy^T) Q(x^T)^T      blocks along the batch
+    """
+
+    def __init__(self, out_features: int, in_features: int, rounding="nearest", grad_rounding="stochastic", seed=0,
+                 device="cuda"):
+        lib.rounding_of(rounding), lib.rounding_of(grad_rounding)
+        self.out_features, self.in_features = out_features, in_features
+        self.rounding, self.grad_rounding, self.seed = rounding, grad_rounding, seed
+        self.by_rows = Mx4Matrix(out_features, in_features, device)
+        self.by_columns = Mx4Matrix(in_features, out_features, device)
+
+    def load(self, weight, step=0):
+        """weight [out_features, in_features], full precision."""
+        quantize_both(weight, self.rounding, self.seed, step, (self.by_rows, self.by_columns))
+
+    def forward(self, x):
+        return linear(x, self.by_rows)
+
+    def forward_train(self, x, step=0):
+        """(y, what backward needs of x: its 4-bit form along the batch)."""
+        rows, saved = quantize_both(x, self.rounding, self.seed, step)
+        return matmul(rows, self.by_rows, x.dtype), saved
+
+    def backward(self, dy, saved: Mx4Matrix, step=0, weight_grad_dtype=torch.float32):
+        """(dx in the type of dy, dw [out_features, in_features])."""
+        rows, cols = quantize_both(dy, self.grad_rounding, self.seed, step)
+        return matmul(rows, self.by_columns, dy.dtype), matmul(cols, saved, weight_grad_dtype)
