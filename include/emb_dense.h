@@ -29,7 +29,8 @@
  * the 16 bytes at 16 (16 b + r) are block b (0..3) of row r, columns in order, the
  * even column in the low half of a byte.  The scale bytes follow, for each row tile
  * and each four column tiles 256 bytes: byte 4 (16 b + r) + t for block b, row r of
- * column tile t.  Codes past the last row or column are 0.
+ * column tile t.  Codes past the last row or column and scale bytes past the last column
+ * tile are 0.
  */
 #ifndef EMB_DENSE_H
 #define EMB_DENSE_H
@@ -71,7 +72,7 @@ int emb_mx4_pack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int6
 int emb_mx4_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, void* stream);
 
 /* c [m][n] (row stride ldc, in elements) = a b^T for MX4 matrices a [m][k] and
- * b [n][k]: products and sums in FP32, one rounding to `type` (nearest even); zeros
+ * b [n][k], k <= 2^24: products and sums in FP32, one rounding to `type` (nearest even); zeros
  * for k = 0.  workspace: emb_mx4_matmul_workspace bytes, 256-byte aligned, or NULL when
  * that is 0.  The order of the sums is a function of m, n and k alone.  Enqueue-only. */
 int emb_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);

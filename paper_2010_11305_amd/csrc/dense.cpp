@@ -28,6 +28,9 @@ bool dims_ok(int64_t rows, int64_t cols) {
   return (double)(rows + kTileRows) * (double)(cols + kTileCols * kScaleTiles) <= kMaxBytes;
 }
 
+// The operands of a product.
+bool product_ok(int64_t m, int64_t n, int64_t k) { return dims_ok(m, k) && dims_ok(n, k) && k <= kMaxDepth; }
+
 // A full-precision matrix: element-aligned, rows not overlapping, inside the address space.
 bool matrix_ok(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld) {
   if (!x || reinterpret_cast<uintptr_t>(x) % type_bytes(type) || ld < cols) return false;
@@ -132,14 +135,14 @@ int emb_mx4_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* codes, ui
 }
 
 int emb_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
-  if (!bytes || !dims_ok(m, k) || !dims_ok(n, k)) return EMB_EINVAL;
+  if (!bytes || !product_ok(m, n, k)) return EMB_EINVAL;
   *bytes = m && n && k ? matmul_workspace(m, n, k) : 0;
   return EMB_OK;
 }
 
 int emb_mx4_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* c, int32_t type, int64_t ldc,
                    void* workspace, size_t workspace_bytes, void* stream) {
-  if (!type_ok(type) || !dims_ok(m, k) || !dims_ok(n, k)) return EMB_EINVAL;
+  if (!type_ok(type) || !product_ok(m, n, k)) return EMB_EINVAL;
   if (m == 0 || n == 0) return EMB_OK;
   if (!matrix_ok(c, type, m, n, ldc)) return EMB_EINVAL;
   if (k && (!a || !b || !aligned(a) || !aligned(b))) return EMB_EINVAL;
@@ -150,14 +153,14 @@ int emb_mx4_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k
 }
 
 int emb_mx4_linear_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
-  if (!bytes || !dims_ok(m, k) || !dims_ok(n, k)) return EMB_EINVAL;
+  if (!bytes || !product_ok(m, n, k)) return EMB_EINVAL;
   *bytes = m && n && k ? linear_workspace(m, n, k) : 0;
   return EMB_OK;
 }
 
 int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                    int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!type_ok(type) || !dims_ok(m, k) || !dims_ok(n, k)) return EMB_EINVAL;
+  if (!type_ok(type) || !product_ok(m, n, k)) return EMB_EINVAL;
   if (m == 0 || n == 0) return EMB_OK;
   if (!matrix_ok(y, type, m, n, ldy)) return EMB_EINVAL;
   if (k && (!matrix_ok(x, type, m, k, ldx) || !w || !aligned(w))) return EMB_EINVAL;

@@ -42,6 +42,7 @@ struct Mx4 {
 };
 
 constexpr int64_t kMaxDim = (int64_t)1 << 31;  // rows and columns stay below it
+constexpr int64_t kMaxDepth = (int64_t)1 << 24;  // columns of a product's operands: offsets inside 8 row tiles fit 31 bits
 // no device memory holds a matrix of more bytes; the tile counts of smaller ones fit a grid
 constexpr double kMaxBytes = (double)((int64_t)1 << 40);
 

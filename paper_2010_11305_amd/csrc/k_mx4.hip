@@ -7,6 +7,15 @@ namespace embd {
 
 namespace {
 
+// The scale byte of a block; with those of the last column tile, zeros for the tiles that its
+// group lacks (a product may run over them).
+__device__ __forceinline__ void store_scale(uint8_t* out, const Mx4& q, int64_t rt, int64_t kt, int lane, uint32_t s) {
+  uint8_t* p = out + q.scale(rt, kt, lane);
+  *p = (uint8_t)s;
+  if (kt + 1 == q.col_tiles)
+    for (int t = (int)(kt % kScaleTiles) + 1; t < kScaleTiles; ++t) *++p = 0;
+}
+
 // By rows: a wave takes one tile, lane 16 b + r quantises block b of row r by itself (no
 // step crosses lanes), and the wave writes the tile's 1024 bytes as they lie.
 template <int TYPE, bool STOCHASTIC>
@@ -23,7 +32,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const typename Elem<TYPE>
   uint32_t s;
   const uint4 c = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
   *reinterpret_cast<uint4*>(out + q.tile(rt, kt) + 16 * lane) = c;
-  out[q.scale(rt, kt, lane)] = (uint8_t)s;
+  store_scale(out, q, rt, kt, lane, s);
 }
 
 // By columns, and by rows from the same pass: a workgroup stages 128 rows x 64 columns in
@@ -64,7 +73,7 @@ __global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TY
       const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)((row0 + b * kBlock) / 8), (uint32_t)col, q, &s);
       const int lane = b * 16 + (int)(col % kTileRows);
       *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
-      by_columns[qc.scale(rt, kt, lane)] = (uint8_t)s;
+      store_scale(by_columns, qc, rt, kt, lane, s);
     }
   }
   if constexpr (ROWS) {
@@ -82,11 +91,11 @@ __global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TY
       const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
       const int lane = (int)(col % kTileCols / kBlock) * 16 + (int)(row % kTileRows);
       *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * lane) = code;
-      by_rows[qr.scale(rt, kt, lane)] = (uint8_t)s;
+      store_scale(by_rows, qr, rt, kt, lane, s);
       // the tile's other half, where no column of x is left for a workgroup of its own
       if (col0 + kStageCols >= qr.cols && col0 % kTileCols == 0) {
         *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * (lane + 32)) = make_uint4(0, 0, 0, 0);
-        by_rows[qr.scale(rt, kt, lane + 32)] = 0;
+        store_scale(by_rows, qr, rt, kt, lane + 32, 0);
       }
     }
   }
@@ -154,7 +163,7 @@ __global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes,
     w[i / 4] |= b << (8 * (i % 4));
   }
   *reinterpret_cast<uint4*>(out + q.tile(rt, kt) + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-  out[q.scale(rt, kt, lane)] = n > 0 ? scales[row * blocks + col / kBlock] : (uint8_t)0;
+  store_scale(out, q, rt, kt, lane, n > 0 ? scales[row * blocks + col / kBlock] : 0u);
 }
 
 __global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {

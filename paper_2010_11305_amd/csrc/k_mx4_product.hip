@@ -1,4 +1,6 @@
 // Products of MX4 matrices on the scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4.
+#include <type_traits>
+
 #include "dense_device.h"
 
 namespace embd {
@@ -6,18 +8,41 @@ namespace embd {
 namespace {
 
 using v8i = int __attribute__((ext_vector_type(8)));
+using v4i = int __attribute__((ext_vector_type(4)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ v8i operand(const uint4& q) {
-  v8i r = {(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0};
-  return r;
+// acc += b a over 128 columns with scale byte S of sb and sa.  IN_PLACE: the instruction is written
+// out with the accumulator tied to its registers.  With 256 of them the register allocator
+// otherwise moves accumulators about between the steps (752 moves for 256 products).  The
+// values it reads come from LDS long before; whoever reads acc waits with mma_done.
+template <int S, bool IN_PLACE>
+__device__ __forceinline__ void mma(f32x4& acc, const v4i& b, const v4i& a, uint32_t sb, uint32_t sa) {
+  if constexpr (IN_PLACE) {
+#define EMBD_MMA(SEL)                                                                                       \
+  asm("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " SEL " cbsz:4 blgp:4"                       \
+      : "+a"(acc)                                                                                           \
+      : "v"(b), "v"(a), "v"(sb), "v"(sa))
+    if constexpr (S == 0) EMBD_MMA("op_sel:[0,0,0] op_sel_hi:[0,0,0]");
+    if constexpr (S == 1) EMBD_MMA("op_sel:[1,1,0] op_sel_hi:[0,0,0]");
+    if constexpr (S == 2) EMBD_MMA("op_sel:[0,0,0] op_sel_hi:[1,1,0]");
+    if constexpr (S == 3) EMBD_MMA("op_sel:[1,1,0] op_sel_hi:[1,1,0]");
+#undef EMBD_MMA
+  } else {
+    const v8i b8 = {b[0], b[1], b[2], b[3]}, a8 = {a[0], a[1], a[2], a[3]};
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b8, a8, acc, 4, 4, S, (int)sb, S, (int)sa);
+  }
 }
 
-// D += A B for one 16x16 tile over 128 columns.  The rows of C are the columns of D (the
-// weight is the first operand), so that a lane holds four consecutive columns of a row of C.
-__device__ __forceinline__ f32x4 mma(const v8i& b, const v8i& a, f32x4 c, uint32_t sb, uint32_t sa) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 4, 4, 0, (int)sb, 0, (int)sa);
+// Wait states between the last matrix instruction and the first read of its result (at most 18); nothing is
+// moved across.
+__device__ __forceinline__ void mma_done() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" : : : "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
+
+// The rows of C are the columns of an instruction's result (b is its first operand), so that a
+// lane holds four consecutive columns of a row of C.
 
 // Columns [col, col + 4) of one row of C.
 template <int TYPE>
@@ -46,35 +71,159 @@ __device__ __forceinline__ void store4(typename Elem<TYPE>::type* row, int64_t c
   }
 }
 
-// A wave computes 32 x 32 of C, its operands straight from memory.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_product(Mx4 a, Mx4 b, typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
-  const int64_t wide = (b.row_tiles + 3) / 4;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t mt = (int64_t)blockIdx.x / wide * 4 + (wave >> 1) * 2, nt = (int64_t)blockIdx.x % wide * 4 + (wave & 1) * 2;
-  if (mt >= a.row_tiles || nt >= b.row_tiles) return;
-  const int64_t ms[2] = {mt, mt + 1 < a.row_tiles ? mt + 1 : mt}, ns[2] = {nt, nt + 1 < b.row_tiles ? nt + 1 : nt};
-  f32x4 acc[2][2] = {};
-  for (int64_t kt = 0; kt < a.col_tiles; ++kt) {
-    v8i fa[2], fb[2];
-    uint32_t sa[2], sb[2];
+// ---- tiles staged through LDS ---------------------------------------------------------------
+using Srd = int __attribute__((ext_vector_type(4)));
+
+// A buffer descriptor over the bytes from p on.  Callers keep every offset inside the matrix
+// themselves: the scalar part of an offset takes no part in the hardware's range check.
+__device__ __forceinline__ Srd make_srd(const uint8_t* p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  Srd r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+           __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)), -1, 0x00020000};
+  return r;
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// 16 bytes a lane from memory into LDS at lds + 16 lane, without registers between.  The
+// compiler does not count it: stage_ready waits for it.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t lane_offset, const Srd& srd, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(lds), "v"(lane_offset), "s"(srd), "s"(offset)
+               : "memory");
+}
+
+// All but the last IN_FLIGHT of the wave's loads to LDS have arrived, and its reads of LDS are
+// done; then the workgroup meets: every wave sees the stage, and the one read before may
+// be overwritten.
+template <int IN_FLIGHT>
+__device__ __forceinline__ void stage_ready() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(IN_FLIGHT) : "memory");
+}
+
+constexpr int kStages = 4;  // one per tile column of a scale group: the loop's body is four steps
+
+// A workgroup of 2 x 2 waves computes (32 FM) x (32 FN) of C, a wave FM x FN tiles of 16 x 16.
+template <int TYPE, int FM, int FN>
+__global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
+                                                                 typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
+  static_assert(FM == FN, "a wave loads tiles of one operand");
+  constexpr int kTiles = 2 * FM + 2 * FN;       // of a stage
+  constexpr int kLoads = kTiles / 4;            // a wave's share of them
+  constexpr int kScaleLoads = FM >= 4 ? FM / 4 : 1;   // 4 row tiles each
+  __shared__ v4i stage[kStages][kTiles][64];
+  __shared__ uint32_t scales[2][kTiles][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  // Workgroups go to the XCDs in turn.  Each XCD takes a run of consecutive tiles, in bands of 8 tile rows, so that what
+  // its L2 holds is used by the workgroups that run there together.
+  const int64_t mt_all = (a.row_tiles + 2 * FM - 1) / (2 * FM), nt_all = (b.row_tiles + 2 * FN - 1) / (2 * FN);
+  const int64_t total = mt_all * nt_all;
+  const int64_t per = total / 8, more = total % 8, xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
+  const int64_t id = xcd * per + (xcd < more ? xcd : more) + nth;
+  const int64_t band = id / (8 * nt_all), in_band = id % (8 * nt_all);
+  const int64_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
+  const int64_t mt = band * 8 + in_band % band_rows, nt = in_band / band_rows;
+  const int64_t rt_a = mt * 2 * FM, rt_b = nt * 2 * FN;
+
+  const int KT = (int)a.col_tiles, KG = (int)a.col_groups;
+  const bool of_a = wave < 2;
+  const Mx4& mine = of_a ? a : b;
+  // Row tiles past the last one are read from it: their products are not stored.
+  const auto row_tile = [&](int64_t rt) { return rt < mine.row_tiles ? rt : mine.row_tiles - 1; };
+  const int64_t rt0 = row_tile((of_a ? rt_a : rt_b) + (wave & 1) * kLoads);   // first row tile that this wave loads
+  const Srd codes = make_srd(mine.base + mine.tile(rt0, 0));
+  uint32_t code_at[kLoads];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      fa[i] = operand(*reinterpret_cast<const uint4*>(a.base + a.tile(ms[i], kt) + 16 * lane));
-      fb[i] = operand(*reinterpret_cast<const uint4*>(b.base + b.tile(ns[i], kt) + 16 * lane));
-      sa[i] = a.base[a.scale(ms[i], kt, lane)];
-      sb[i] = b.base[b.scale(ns[i], kt, lane)];
+  for (int i = 0; i < kLoads; ++i) code_at[i] = (uint32_t)(row_tile(rt0 + i) - rt0) * (uint32_t)KT * kTileBytes + lane * 16;
+  const int64_t rs0 = row_tile((of_a ? rt_a : rt_b) + (FM >= 4 ? (wave & 1) * FM : 0));
+  const Srd scale_srd = make_srd(mine.base + mine.scale_offset + rs0 * KG * kScaleBytes);
+  uint32_t scale_at[kScaleLoads];   // 4 row tiles a load, 16 lanes each
+#pragma unroll
+  for (int i = 0; i < kScaleLoads; ++i)
+    scale_at[i] = (uint32_t)(row_tile(rs0 + 4 * i + (lane >> 4)) - rs0) * (uint32_t)KG * kScaleBytes + (lane & 15) * 16;
+  const uint32_t stage_at = lds_address(&stage[0][wave * kLoads][0]);
+  const uint32_t scales_at = lds_address(&scales[0][(of_a ? 0 : 2 * FM) + (FM >= 4 ? (wave & 1) * FM : 0)][0]);
+
+  // Column tiles past the last one are loaded from it again, so that the number of loads in flight
+  // stays the same; the steps of the last group that run over them have scale bytes 0 on both
+  // sides, 2^-254 of whatever finite codes are there, which FP32 sums do not see.
+  const auto load_part = [&](int kt, int i) {
+    const int k = kt < KT ? kt : KT - 1;
+    load_to_lds(stage_at + (kt % kStages) * (kTiles * 1024) + i * 1024, code_at[i], codes, k * kTileBytes);
+  };
+  const auto load_stage = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_part(kt, i);
+  };
+  const auto load_scales = [&](int kg) {
+    const int k = kg < KG ? kg : KG - 1;
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i)
+      load_to_lds(scales_at + (kg % 2) * (kTiles * 256) + i * 1024, scale_at[i], scale_srd, k * kScaleBytes);
+  };
+
+  f32x4 acc[FM][FN] = {};
+  v4i fa[2][FM], fb[2][FN];
+  uint32_t sa[FM], sb[FN], sna[FM], snb[FN];
+  load_scales(0);
+  load_stage(0);
+  load_stage(1);
+  load_stage(2);
+  load_stage(3);
+  stage_ready<3 * kLoads>();
+#pragma unroll
+  for (int i = 0; i < FM; ++i) fa[0][i] = stage[0][wm * FM + i][lane], sa[i] = scales[0][wm * FM + i][lane];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) fb[0][j] = stage[0][2 * FM + wn * FN + j][lane], sb[j] = scales[0][2 * FM + wn * FN + j][lane];
+
+  // Step kt: wait for stage kt + 1, let stage kt + 4 be loaded over stage kt (in registers since
+  // the step before), read stage kt + 1 while the products of stage kt run.  The loads and
+  // reads are spread over the products, a row of FN of them at a time: left alone, the
+  // compiler puts the reads behind them all, and the next step waits for LDS.
+  const auto step = [&](auto S, int kt) {
+    constexpr int s = decltype(S)::value, cur = s & 1, nxt = cur ^ 1;
+    // in flight behind stage kt + 1: two later stages, and between them the scales of a step 0
+    stage_ready<2 * kLoads + (s == 1 || s == 2 ? kScaleLoads : 0)>();
+    if constexpr (s == 0) load_scales(kt / 4 + 1);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (i < kLoads) load_part(kt + 4, i);
+      fa[nxt][i] = stage[(s + 1) % kStages][wm * FM + i][lane];
+      fb[nxt][i] = stage[(s + 1) % kStages][2 * FM + wn * FN + i][lane];
+      if constexpr (s == 3) {
+        sna[i] = scales[(kt / 4 + 1) % 2][wm * FM + i][lane];
+        snb[i] = scales[(kt / 4 + 1) % 2][2 * FM + wn * FN + i][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) mma<s, FM == 8>(acc[i][j], fb[cur][j], fa[cur][i], sb[j], sa[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (s == 3) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
+      for (int i = 0; i < FM; ++i) sa[i] = sna[i], sb[i] = snb[i];
+    }
+  };
+  for (int kt = 0; kt < KT; kt += kStages) {
+    step(std::integral_constant<int, 0>{}, kt);
+    step(std::integral_constant<int, 1>{}, kt + 1);
+    step(std::integral_constant<int, 2>{}, kt + 2);
+    step(std::integral_constant<int, 3>{}, kt + 3);
+    if (FM == 8 && kt + kStages >= KT) mma_done();
   }
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load to LDS outlives the workgroup
+
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int64_t row = (mt + i) * kTileRows + (lane & 15), col = (nt + j) * kTileRows + (lane >> 4) * 4;
+    for (int j = 0; j < FN; ++j) {
+      const int64_t row = (rt_a + wm * FM + i) * kTileRows + (lane & 15);
+      const int64_t col = (rt_b + wn * FN + j) * kTileRows + (lane >> 4) * 4;
       if (row < a.rows && col < b.rows) store4<TYPE>(c + row * ldc, col, b.rows, acc[i][j]);
     }
 }
@@ -95,8 +244,14 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
     return hipGetLastError();
   }
   const Mx4 qa(a, m, k), qb(b, n, k);
-  const int64_t grid = ((qa.row_tiles + 3) / 4) * ((qb.row_tiles + 3) / 4);
-  k_product<TYPE><<<(unsigned)grid, 256, 0, s>>>(qa, qb, c, ldc);
+  const auto tiles = [&](int f) { return ((qa.row_tiles + 2 * f - 1) / (2 * f)) * ((qb.row_tiles + 2 * f - 1) / (2 * f)); };
+  const int f = tiles(8) >= 192 ? 8 : tiles(4) >= 192 ? 4 : 2;
+  if (f == 8)
+    k_product<TYPE, 8, 8><<<(unsigned)tiles(8), 256, 0, s>>>(qa, qb, c, ldc);
+  else if (f == 4)
+    k_product<TYPE, 4, 4><<<(unsigned)tiles(4), 256, 0, s>>>(qa, qb, c, ldc);
+  else
+    k_product<TYPE, 2, 2><<<(unsigned)tiles(2), 256, 0, s>>>(qa, qb, c, ldc);
   return hipGetLastError();
 }
 
