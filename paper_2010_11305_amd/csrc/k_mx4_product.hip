@@ -192,17 +192,19 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
     if constexpr (s == 0) load_scales(kt / 4 + 1);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      if (i < kLoads) load_part(kt + 4, i);
-      fa[nxt][i] = stage[(s + 1) % kStages][wm * FM + i][lane];
-      fb[nxt][i] = stage[(s + 1) % kStages][2 * FM + wn * FN + i][lane];
-      if constexpr (s == 3) {
-        sna[i] = scales[(kt / 4 + 1) % 2][wm * FM + i][lane];
-        snb[i] = scales[(kt / 4 + 1) % 2][2 * FM + wn * FN + i][lane];
-      }
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) mma<s, FM == 8>(acc[i][j], fb[cur][j], fa[cur][i], sb[j], sa[i]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < FN; ++j) {
+        mma<s, FM == 8>(acc[i][j], fb[cur][j], fa[cur][i], sb[j], sa[i]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (j == FN / 4 - (FN == 2 ? 0 : 1)) fa[nxt][i] = stage[(s + 1) % kStages][wm * FM + i][lane];
+        if (j == FN / 2 - 1) fb[nxt][i] = stage[(s + 1) % kStages][2 * FM + wn * FN + i][lane];
+        if (j == 3 * FN / 4 - 1 && i < kLoads) load_part(kt + 4, i);
+        if (s == 3 && j == FN - 1) {
+          sna[i] = scales[(kt / 4 + 1) % 2][wm * FM + i][lane];
+          snb[i] = scales[(kt / 4 + 1) % 2][2 * FM + wn * FN + i][lane];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     if constexpr (s == 3) {
 #pragma unroll
@@ -216,14 +218,50 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
     step(std::integral_constant<int, 3>{}, kt + 3);
     if (FM == 8 && kt + kStages >= KT) mma_done();
   }
-  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load to LDS outlives the workgroup
+  stage_ready<0>();  // no load to LDS is on its way, and no wave reads a stage any more
 
+  // A wave's part of C, when it lies inside: through LDS, rows of whole lines out of it.  Else element by element.
+  const int64_t row0 = (rt_a + wm * FM) * kTileRows, col0 = (rt_b + wn * FN) * kTileRows;
+  if (row0 + FM * 16 <= a.rows && col0 + FN * 16 <= b.rows) {
+    constexpr int kBytes = Elem<TYPE>::kBytes, kPitch = FN * 16 * kBytes + 16;
+    constexpr int kRound = TYPE == EMB_TYPE_FP32 && FM > 2 ? FM / 4 : FM / 2;   // row tiles at a time
+    constexpr int kLanes = FN * 16 * kBytes / 16, kRows = 64 / kLanes;  // lanes a row, rows an access
+    static_assert(4 * kRound * 16 * kPitch <= (int)sizeof(stage));
+    uint8_t* own = reinterpret_cast<uint8_t*>(&stage[0][0][0]) + wave * (kRound * 16 * kPitch);
+    typename Elem<TYPE>::type* out = c + (row0 + lane / kLanes) * ldc + col0 + lane % kLanes * (16 / kBytes);
+#pragma unroll
+    for (int r = 0; r < FM; r += kRound) {
+#pragma unroll
+      for (int i = 0; i < kRound; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          uint8_t* p = own + (i * 16 + (lane & 15)) * kPitch + (j * 16 + (lane >> 4) * 4) * kBytes;
+          const f32x4 v = acc[r + i][j];
+          if constexpr (TYPE == EMB_TYPE_FP32)
+            *reinterpret_cast<f32x4*>(p) = v;
+          else
+            *reinterpret_cast<uint2*>(p) = make_uint2(to_bits<TYPE>(v[0]) | to_bits<TYPE>(v[1]) << 16,
+                                                      to_bits<TYPE>(v[2]) | to_bits<TYPE>(v[3]) << 16);
+        }
+      asm volatile("" : : : "memory");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < kRound * 16; i += kRows) {
+        const v4i v = *reinterpret_cast<const v4i*>(own + (i + lane / kLanes) * kPitch + lane % kLanes * 16);
+        const Bytes16 w = {{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]}};
+        *reinterpret_cast<Bytes16*>(out + (r * 16 + i) * ldc) = w;
+      }
+      asm volatile("" : : : "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-      const int64_t row = (rt_a + wm * FM + i) * kTileRows + (lane & 15);
-      const int64_t col = (rt_b + wn * FN + j) * kTileRows + (lane >> 4) * 4;
+      const int64_t row = row0 + i * kTileRows + (lane & 15);
+      const int64_t col = col0 + j * kTileRows + (lane >> 4) * 4;
       if (row < a.rows && col < b.rows) store4<TYPE>(c + row * ldc, col, b.rows, acc[i][j]);
     }
 }
