@@ -73,17 +73,15 @@ int emb_mx4_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* codes, ui
 
 /* c [m][n] (row stride ldc, in elements) = a b^T for MX4 matrices a [m][k] and
  * b [n][k], k <= 2^24: products and sums in FP32, one rounding to `type` (nearest even); zeros
- * for k = 0.  workspace: emb_mx4_matmul_workspace bytes, 256-byte aligned, or NULL when
- * that is 0.  The order of the sums is a function of m, n and k alone.  Enqueue-only. */
-int emb_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
+ * for k = 0.  The order of the sums is a function of m, n and k alone.  Enqueue-only. */
 int emb_mx4_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* c, int32_t type, int64_t ldc,
-                   void* workspace, size_t workspace_bytes, void* stream);
+                   void* stream);
 
 /* The linear layer: y [m][n] = Q(x) w^T for full-precision rows x [m][k] (row stride
  * ldx), quantised to nearest on the way, and an MX4 weight w [n][k]; y in the type of
  * x, row stride ldy.  Equal to emb_mx4_quantize of x and emb_mx4_matmul up to the order
- * of the FP32 sums.  workspace as for the product, emb_mx4_linear_workspace bytes.
- * Enqueue-only. */
+ * of the FP32 sums.  workspace: emb_mx4_linear_workspace bytes, 256-byte aligned, or NULL
+ * when that is 0.  Enqueue-only. */
 int emb_mx4_linear_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
 int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                    int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);

@@ -8,6 +8,7 @@ Parameters are updated in place.  The update runs in one HIP kernel per 192 tens
 from __future__ import annotations
 
 import ctypes
+from array import array
 
 import torch
 
@@ -51,10 +52,10 @@ class AdamW:
         lib.check(L.emb_adamw_query_sizes(ctypes.byref(c), ctypes.byref(self._layout)), "emb_adamw_query_sizes")
         self.state_buffer = torch.empty(max(self._layout.state_bytes, 256), dtype=torch.uint8, device=self.device)
         self._h = ctypes.c_void_p()
-        with lib.on_device(self.device):
+        with torch.cuda.device(self.device):
             lib.check(L.emb_adamw_create(ctypes.byref(c), self.state_buffer.data_ptr(), self._layout.state_bytes,
-                                         lib.stream(self.device), ctypes.byref(self._h)), "emb_adamw_create")
-        self._pointers = ctypes.c_void_p * n
+                                         torch.cuda.current_stream().cuda_stream, ctypes.byref(self._h)),
+                      "emb_adamw_create")
 
     def close(self):
         if getattr(self, "_h", None):
@@ -73,23 +74,19 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
-        gp, gd, dev = [], self.grad_dtype, self.device
+        gd, index = self.grad_dtype, self.device.index
         for g, n in zip(grads, self.sizes):
-            if g is None:
-                gp.append(None)
-                continue
-            if g.dtype != gd or g.numel() != n or g.device != dev or not g.is_contiguous():
-                raise ValueError(f"a gradient must be contiguous, {gd}, on {dev}, and as large as its parameter")
-            gp.append(g.data_ptr())
+            if g is not None and (g.dtype != gd or g.numel() != n or g.get_device() != index or not g.is_contiguous()):
+                raise ValueError(f"a gradient must be contiguous, {gd}, on {self.device}, and as large as its parameter")
         scale = None
         if grad_scale is not None:
-            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
-                raise ValueError(f"grad_scale must be one float32 value on {dev}")
+            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != index:
+                raise ValueError(f"grad_scale must be one float32 value on {self.device}")
             scale = grad_scale.data_ptr()
-        with lib.on_device(dev):
-            lib.check(lib.load().emb_adamw_step(self._h, self._pointers(*[p.data_ptr() for p in self.params]),
-                                                self._pointers(*gp), self.lr if lr is None else float(lr), scale,
-                                                lib.stream(dev)), "emb_adamw_step")
+        pp = array("Q", [p.data_ptr() for p in self.params])
+        gp = array("Q", [0 if g is None else g.data_ptr() for g in grads])
+        lib.call("emb_adamw_step", self.device, self._h, pp.buffer_info()[0], gp.buffer_info()[0],
+                 self.lr if lr is None else float(lr), scale)
 
     def state(self) -> dict:
         """The moments, as views of the state buffer over all tensors, each tensor's part padded to a multiple of 32

@@ -177,9 +177,10 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
   load_stage(3);
   stage_ready<3 * kLoads>();
 #pragma unroll
-  for (int i = 0; i < FM; ++i) fa[0][i] = stage[0][wm * FM + i][lane], sa[i] = scales[0][wm * FM + i][lane];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) fb[0][j] = stage[0][2 * FM + wn * FN + j][lane], sb[j] = scales[0][2 * FM + wn * FN + j][lane];
+  for (int i = 0; i < FM; ++i) {
+    fa[0][i] = stage[0][wm * FM + i][lane], sa[i] = scales[0][wm * FM + i][lane];
+    fb[0][i] = stage[0][2 * FM + wn * FN + i][lane], sb[i] = scales[0][2 * FM + wn * FN + i][lane];
+  }
 
   // Step kt: wait for stage kt + 1, let stage kt + 4 be loaded over stage kt (in registers since
   // the step before), read stage kt + 1 while the products of stage kt run.  The loads and
@@ -266,15 +267,174 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
     }
 }
 
+// ---- few rows ---------------------------------------------------------------------------------
+// One operand (x) has few rows: a workgroup takes 16 MT of them (blockIdx.y) and 16 of the other (w), and its
+// waves share the columns: a wave takes one group of four column tiles at a time straight into
+// registers (4 KB, with the next one already on its way) and the waves' sums meet in LDS, in
+// the order of the waves.  XT >= 0: x is a full-precision matrix that every workgroup
+// quantises into LDS first, 32 values a thread, while the first group of w arrives.
+constexpr int kSkinnyWaves = 16;
+constexpr int kFusedValues = 32768;   // of x, most
+
+struct FullRows {
+  const void* x;
+  int64_t ld;
+};
+
+template <int XT, int TYPE, int MT, bool SWAP>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(Mx4 w, Mx4 x, FullRows full,
+                                                              typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
+  constexpr bool kFused = XT >= 0;
+  __shared__ f32x4 sums[kSkinnyWaves][MT][64];
+  __shared__ uint4 codes[kFused ? kFusedValues / kBlock : 1];
+  __shared__ uint32_t code_scales[kFused ? kFusedValues / kBlock / 4 : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t rt = blockIdx.x;
+  const int KT = (int)w.col_tiles, KG = (int)w.col_groups;
+  const int64_t x_tile0 = (int64_t)blockIdx.y * MT;
+  const int m = (int)(x.rows - x_tile0 * kTileRows < MT * kTileRows ? x.rows - x_tile0 * kTileRows : MT * kTileRows);
+
+  v4i next[4];
+  uint32_t next_scale;
+  const auto fetch = [&](int kg) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int kt = kg * 4 + t < KT ? kg * 4 + t : KT - 1;   // past the end: scale byte 0
+      next[t] = *reinterpret_cast<const v4i*>(w.base + w.tile(rt, kt) + 16 * lane);
+    }
+    next_scale = *reinterpret_cast<const uint32_t*>(w.base + w.scale_offset + (rt * KG + kg) * kScaleBytes + 4 * lane);
+  };
+  if (wave < KG) fetch(wave);
+
+  if constexpr (kFused) {
+    // block b of row r of column tile kt at (4 kt + b) m + r; its scale byte in byte kt % 4 of a dword
+    const auto* px = static_cast<const typename Elem<XT>::type*>(full.x);
+    for (int id = threadIdx.x; id < KG * 16 * m; id += blockDim.x) {
+      const int r = id % m, block = id / m;
+      const int64_t left = x.cols - (int64_t)block * kBlock;
+      Raw<XT, kBlock> v;
+      load_values(px + (left > 0 ? r * full.ld + (int64_t)block * kBlock : 0), (int)(left < 0 ? 0 : left > kBlock ? kBlock : left), v);
+      uint32_t s;
+      codes[id] = quantize_block<XT, false>(v, 0, 0, Mx4Random{}, &s);
+      const int kt = block / 4, b = block % 4;
+      reinterpret_cast<uint8_t*>(code_scales)[4 * ((kt / 4 * 4 + b) * m + r) + kt % 4] = (uint8_t)s;
+    }
+    __syncthreads();
+  }
+
+  f32x4 acc[MT] = {};
+  for (int kg = wave; kg < KG; kg += waves) {
+    v4i cur[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) cur[t] = next[t];
+    const uint32_t scale = next_scale;
+    if (kg + waves < KG) fetch(kg + waves);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int row = i * 16 + (lane & 15), b = lane >> 4;
+      if (i * 16 >= m) break;
+      v4i xf[4];
+      uint32_t xs;
+      if constexpr (kFused) {
+        const bool in = row < m;
+        xs = in ? code_scales[(kg * 4 + b) * m + row] : 0u;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          xf[t] = v4i{0, 0, 0, 0};
+          if (in) xf[t] = __builtin_bit_cast(v4i, codes[((kg * 4 + t) * 4 + b) * m + row]);
+        }
+      } else {
+        xs = *reinterpret_cast<const uint32_t*>(x.base + x.scale_offset + ((x_tile0 + i) * KG + kg) * kScaleBytes + 4 * lane);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int kt = kg * 4 + t < KT ? kg * 4 + t : KT - 1;
+          xf[t] = *reinterpret_cast<const v4i*>(x.base + x.tile(x_tile0 + i, kt) + 16 * lane);
+        }
+      }
+      mma<0, false>(acc[i], cur[0], xf[0], scale, xs);
+      mma<1, false>(acc[i], cur[1], xf[1], scale, xs);
+      mma<2, false>(acc[i], cur[2], xf[2], scale, xs);
+      mma<3, false>(acc[i], cur[3], xf[3], scale, xs);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+  for (int i = wave; i < MT; i += waves) {
+    if (i * 16 + (lane & 15) >= m) continue;
+    const int64_t row = (x_tile0 + i) * kTileRows + (lane & 15), col = rt * kTileRows + (lane >> 4) * 4;
+    f32x4 v = sums[0][i][lane];
+    for (int k = 1; k < waves; ++k) v = v + sums[k][i][lane];
+    if constexpr (SWAP) {  // the rows of w are those of C
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (col + q >= w.rows) continue;
+        if constexpr (TYPE == EMB_TYPE_FP32)
+          c[(col + q) * ldc + row] = v[q];
+        else
+          c[(col + q) * ldc + row] = (uint16_t)to_bits<TYPE>(v[q]);
+      }
+    } else if (col < w.rows) {
+      store4<TYPE>(c + row * ldc, col, w.rows, v);
+    }
+  }
+}
+
+// Row tiles of a workgroup's x in k_skinny.
+int skinny_tiles(int64_t x_tiles) { return x_tiles <= 1 ? 1 : x_tiles <= 2 ? 2 : 4; }
+
+template <int XT, int TYPE, bool SWAP>
+hipError_t skinny(const Mx4& w, const Mx4& x, const FullRows& full, typename Elem<TYPE>::type* c, int64_t ldc,
+                  hipStream_t s) {
+  // as many rounds of groups as 16 waves need, and no more waves than these rounds do
+  const int64_t rounds = (w.col_groups + kSkinnyWaves - 1) / kSkinnyWaves;
+  const int64_t need = (w.col_groups + rounds - 1) / rounds;
+  const unsigned threads = 64u * (unsigned)(XT >= 0 && need < 4 ? 4 : need);
+  const int mt = skinny_tiles(x.row_tiles);
+  const dim3 grid((unsigned)w.row_tiles, (unsigned)((x.row_tiles + mt - 1) / mt));
+  if (mt == 1)
+    k_skinny<XT, TYPE, 1, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
+  else if (mt == 2)
+    k_skinny<XT, TYPE, 2, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
+  else
+    k_skinny<XT, TYPE, 4, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
+  return hipGetLastError();
+}
+
 // C = 0 (a product over no columns).
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_zero(int64_t m, int64_t n, typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) c[i / n * ldc + i % n] = 0;
 }
 
+// ---- the way of a product ------------------------------------------------------------------------
+int64_t tiles_of(const Mx4& a, const Mx4& b, int f) {
+  return ((a.row_tiles + 2 * f - 1) / (2 * f)) * ((b.row_tiles + 2 * f - 1) / (2 * f));
+}
+
+// k_skinny reads its w once for each 64 rows of x and its x once for each 16 rows of w, all of it from L2 at best: it
+// wins while its workgroups are about as many as the CUs can hold at once, whatever the columns, and for up
+// to 16 rows always.  us, k_skinny against the best of k_product: 300x300x12800 8.6 / 16.1 (95 workgroups of 4
+// tiles), 512x512x4096 5.6 / 7.3 (256), 96x3000x6000 9.7 / 10.3 (376), 32x8192x12800 15.6 / 18.0 (512 of 2 tiles);
+// 200x2000x12800 21.2 / 17.3 (500), 64x8192x12800 21.1 / 18.3 (512), 1024x1024x12800 31.3 / 18.3 (1024).
+bool use_skinny(const Mx4& a, const Mx4& b) {
+  const int64_t x = a.row_tiles < b.row_tiles ? a.row_tiles : b.row_tiles;
+  const int64_t w = a.row_tiles < b.row_tiles ? b.row_tiles : a.row_tiles;
+  const int mt = skinny_tiles(x);
+  return x <= 1 || w * ((x + mt - 1) / mt) * (1 + mt) <= 1920;
+}
+
+// Row tiles of a wave's side in k_product, the side of a workgroup's tile being 32 of them: the least time, in
+// units of a round of 256 workgroups of 256 x 256.  Full rounds (16384x8192x12800): 92 us at f = 8, 28.7 at 4, 10.9
+// at 2; one round alone (1024x1024x12800, 256 CUs not full at 8 and 4): 63, 25 and 18.3.
+int tile_side(const Mx4& a, const Mx4& b) {
+  const auto rounds = [&](int f) { return (double)((tiles_of(a, b, f) + 255) / 256); };
+  const double t8 = rounds(8), t4 = 0.31 * rounds(4) + 0.09, t2 = 0.12 * (rounds(2) + 1);
+  return t8 <= t4 && t8 <= t2 ? 8 : t4 <= t2 ? 4 : 2;
+}
+
 template <int TYPE>
-hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* cv, int64_t ldc,
-                     hipStream_t s) {
+hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* cv, int64_t ldc, hipStream_t s) {
   auto* c = static_cast<typename Elem<TYPE>::type*>(cv);
   if (!k) {
     const int64_t blocks = (m * n + 255) / 256;
@@ -282,40 +442,52 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
     return hipGetLastError();
   }
   const Mx4 qa(a, m, k), qb(b, n, k);
-  const auto tiles = [&](int f) { return ((qa.row_tiles + 2 * f - 1) / (2 * f)) * ((qb.row_tiles + 2 * f - 1) / (2 * f)); };
-  const int f = tiles(8) >= 192 ? 8 : tiles(4) >= 192 ? 4 : 2;
+  if (use_skinny(qa, qb))
+    return qb.row_tiles < qa.row_tiles ? skinny<-1, TYPE, true>(qa, qb, FullRows{}, c, ldc, s)
+                                       : skinny<-1, TYPE, false>(qb, qa, FullRows{}, c, ldc, s);
+  const int f = tile_side(qa, qb);
+  const unsigned grid = (unsigned)tiles_of(qa, qb, f);
   if (f == 8)
-    k_product<TYPE, 8, 8><<<(unsigned)tiles(8), 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 8, 8><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   else if (f == 4)
-    k_product<TYPE, 4, 4><<<(unsigned)tiles(4), 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 4, 4><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   else
-    k_product<TYPE, 2, 2><<<(unsigned)tiles(2), 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 2, 2><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   return hipGetLastError();
 }
 
+// Rows that every workgroup of k_skinny quantises by itself.
+bool fused(int64_t m, int64_t k) { return m <= 64 && m * ((k + 511) / 512 * 512) <= kFusedValues; }
+
 }  // namespace
 
-size_t matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
-
 hipError_t launch_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* c, int type, int64_t ldc,
-                         void* workspace, hipStream_t s) {
+                         hipStream_t s) {
   if (type == EMB_TYPE_FP32) return matmul_as<EMB_TYPE_FP32>(a, b, m, n, k, c, ldc, s);
   if (type == EMB_TYPE_BF16) return matmul_as<EMB_TYPE_BF16>(a, b, m, n, k, c, ldc, s);
   return matmul_as<EMB_TYPE_FP16>(a, b, m, n, k, c, ldc, s);
 }
 
-size_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-  return ((size_t)Mx4(nullptr, m, k).bytes() + 255) / 256 * 256 + matmul_workspace(m, n, k);
+size_t linear_workspace(int64_t m, int64_t k) {
+  return fused(m, k) ? 0 : (size_t)Mx4(nullptr, m, k).bytes();
 }
 
 hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                          int64_t ldy, void* workspace, hipStream_t s) {
+  if (k && fused(m, k)) {
+    const Mx4 qw(w, n, k), qx(nullptr, m, k);
+    const FullRows full = {x, ldx};
+    if (type == EMB_TYPE_FP32)
+      return skinny<EMB_TYPE_FP32, EMB_TYPE_FP32, false>(qw, qx, full, static_cast<float*>(y), ldy, s);
+    if (type == EMB_TYPE_BF16)
+      return skinny<EMB_TYPE_BF16, EMB_TYPE_BF16, false>(qw, qx, full, static_cast<uint16_t*>(y), ldy, s);
+    return skinny<EMB_TYPE_FP16, EMB_TYPE_FP16, false>(qw, qx, full, static_cast<uint16_t*>(y), ldy, s);
+  }
   if (k) {
     const hipError_t e = launch_quantize(x, type, m, k, ldx, workspace, nullptr, EMB_ROUND_NEAREST, 0, 0, s);
     if (e != hipSuccess) return e;
   }
-  const size_t q = k ? ((size_t)Mx4(nullptr, m, k).bytes() + 255) / 256 * 256 : 0;
-  return launch_matmul(workspace, w, m, n, k, y, type, ldy, static_cast<uint8_t*>(workspace) + q, s);
+  return launch_matmul(workspace, w, m, n, k, y, type, ldy, s);
 }
 
 }  // namespace embd

@@ -57,8 +57,7 @@ def load():
         "emb_mx4_dequantize": [P, i64, i64, P, i32, i64, P],
         "emb_mx4_pack": [P, P, i64, i64, P, P],
         "emb_mx4_unpack": [P, i64, i64, P, P, P],
-        "emb_mx4_matmul_workspace": [i64, i64, i64, c.POINTER(size)],
-        "emb_mx4_matmul": [P, P, i64, i64, i64, P, i32, i64, P, size, P],
+        "emb_mx4_matmul": [P, P, i64, i64, i64, P, i32, i64, P],
         "emb_mx4_linear_workspace": [i64, i64, i64, c.POINTER(size)],
         "emb_mx4_linear": [P, i32, i64, i64, i64, P, i64, P, i64, P, size, P],
         "emb_adamw_query_sizes": [c.POINTER(AdamwConfig), c.POINTER(AdamwSizes)],
@@ -81,13 +80,19 @@ def check(status: int, what: str):
         raise emb_cache.EmbCacheError(status, what)
 
 
-def stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def on_device(device):
-    """The device a call runs on made current, where it is not."""
-    return torch.cuda.device(device)
+def call(name: str, device, *args):
+    """One enqueue-only function of the library on the current stream of `device`, which is made current where it
+    is not.  Small operators last a few microseconds, as long as this does: hence torch's raw
+    accessors, and no context manager on the usual way."""
+    f = getattr(_lib or load(), name)
+    index = device.index
+    if torch._C._cuda_getDevice() == index:
+        status = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        raise emb_cache.EmbCacheError(status, name)
 
 
 def rounding_of(name: str) -> int:

@@ -60,14 +60,9 @@ class Mx4Matrix:
 
     def dequantize(self, dtype=torch.float32, out=None):
         """The values as a [rows, cols] tensor (exact in float32 and bfloat16)."""
-        if out is None:
-            out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.data.device)
-        p, t, rows, cols, ld = lib.matrix(out, "out")
-        if (rows, cols) != self.shape or out.device != self.device:
-            raise ValueError(f"out must be {self.shape} on {self.device}")
-        with lib.on_device(self.device):
-            lib.check(lib.load().emb_mx4_dequantize(self.data.data_ptr(), rows, cols, p, t, ld, lib.stream(self.device)),
-                      "emb_mx4_dequantize")
+        rows, cols, dev = self.rows, self.cols, self.data.device
+        out, p, t, ld = _result(out, rows, cols, dtype, dev)
+        lib.call("emb_mx4_dequantize", dev, self.data.data_ptr(), rows, cols, p, t, ld)
         return out
 
     def to_codes(self):
@@ -75,9 +70,8 @@ class Mx4Matrix:
         byte with the even column in the low half: the plain form, for checkpoints and exchange."""
         codes = torch.empty((self.rows, -(-self.cols // 2)), dtype=torch.uint8, device=self.device)
         scales = torch.empty((self.rows, -(-self.cols // 32)), dtype=torch.uint8, device=self.device)
-        with lib.on_device(self.device):
-            lib.check(lib.load().emb_mx4_unpack(self.data.data_ptr(), self.rows, self.cols, codes.data_ptr(),
-                                                scales.data_ptr(), lib.stream(self.device)), "emb_mx4_unpack")
+        lib.call("emb_mx4_unpack", self.device, self.data.data_ptr(), self.rows, self.cols, codes.data_ptr(),
+                 scales.data_ptr())
         return codes, scales
 
 
@@ -88,16 +82,14 @@ def from_codes(codes, scales, cols: int, out: Mx4Matrix | None = None) -> Mx4Mat
         if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != (rows, width):
             raise ValueError(f"{what} must be a contiguous uint8 tensor [{rows}, {width}] on the GPU")
     out = _target(out, rows, cols, codes.device, "out")
-    with lib.on_device(out.device):
-        lib.check(lib.load().emb_mx4_pack(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data.data_ptr(),
-                                          lib.stream(out.device)), "emb_mx4_pack")
+    lib.call("emb_mx4_pack", out.device, codes.data_ptr(), scales.data_ptr(), rows, cols, out.data.data_ptr())
     return out
 
 
 def _target(out, rows, cols, device, what) -> Mx4Matrix:
     if out is None:
         return Mx4Matrix(rows, cols, device)
-    if out.shape != (rows, cols) or out.device != device:
+    if not isinstance(out, Mx4Matrix) or out.shape != (rows, cols) or out.device != device:
         raise ValueError(f"{what} must be an Mx4Matrix [{rows}, {cols}] on {device}")
     return out
 
@@ -107,11 +99,8 @@ def _quantize(x, rows_out, columns_out, rounding, seed, step):
     p, t, rows, cols, ld = lib.matrix(x, "x")
     by_rows = None if rows_out is False else _target(rows_out, rows, cols, x.device, "the matrix by rows")
     by_columns = None if columns_out is False else _target(columns_out, cols, rows, x.device, "the matrix by columns")
-    with lib.on_device(x.device):
-        lib.check(lib.load().emb_mx4_quantize(p, t, rows, cols, ld, by_rows.data.data_ptr() if by_rows else None,
-                                              by_columns.data.data_ptr() if by_columns else None,
-                                              lib.rounding_of(rounding), seed, step, lib.stream(x.device)),
-                  "emb_mx4_quantize")
+    lib.call("emb_mx4_quantize", x.device, p, t, rows, cols, ld, by_rows and by_rows.data.data_ptr(),
+             by_columns and by_columns.data.data_ptr(), lib.rounding_of(rounding), seed, step)
     return by_rows, by_columns
 
 
@@ -131,16 +120,14 @@ def quantize_both(x, rounding="nearest", seed=0, step=0, out=(None, None)):
 
 
 def _result(out, rows, cols, dtype, device):
+    """(out, pointer, type, row stride) of a result [rows, cols], new where none is given."""
     if out is None:
         out = torch.empty((rows, cols), dtype=dtype, device=device)
+        return out, out.data_ptr(), lib.type_of(dtype), max(cols, 1)
     p, t, r, c, ld = lib.matrix(out, "out")
-    if (r, c) != (rows, cols) or out.device != device:
+    if r != rows or c != cols or out.device != device:
         raise ValueError(f"out must be [{rows}, {cols}] on {device}")
     return out, p, t, ld
-
-
-def _workspace(bytes_, device):
-    return torch.empty(bytes_, dtype=torch.uint8, device=device) if bytes_ else None
 
 
 def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
@@ -149,11 +136,7 @@ def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
         raise ValueError(f"a {a.shape} and b {b.shape} must have the same number of columns, on one device")
     dev = a.device
     out, p, t, ld = _result(out, a.rows, b.rows, dtype, dev)
-    need = _query("emb_mx4_matmul_workspace", a.rows, b.rows, a.cols)
-    ws = _workspace(need, dev)
-    with lib.on_device(dev):
-        lib.check(lib.load().emb_mx4_matmul(a.data.data_ptr(), b.data.data_ptr(), a.rows, b.rows, a.cols, p, t, ld,
-                                            ws.data_ptr() if need else None, need, lib.stream(dev)), "emb_mx4_matmul")
+    lib.call("emb_mx4_matmul", dev, a.data.data_ptr(), b.data.data_ptr(), a.rows, b.rows, a.cols, p, t, ld)
     return out
 
 
@@ -167,10 +150,8 @@ def linear(x, w: Mx4Matrix, out=None):
     if yt != t:
         raise ValueError("out must have the type of x")
     need = _query("emb_mx4_linear_workspace", m, w.rows, k)
-    ws = _workspace(need, dev)
-    with lib.on_device(dev):
-        lib.check(lib.load().emb_mx4_linear(p, t, m, k, ld, w.data.data_ptr(), w.rows, yp, yld,
-                                            ws.data_ptr() if need else None, need, lib.stream(dev)), "emb_mx4_linear")
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    lib.call("emb_mx4_linear", dev, p, t, m, k, ld, w.data.data_ptr(), w.rows, yp, yld, ws.data_ptr() if need else None, need)
     return out
 
 

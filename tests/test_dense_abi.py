@@ -28,7 +28,7 @@ def L():
 def test_every_declared_symbol_is_exported(L):
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "emb_dense.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(emb_(?:mx4|adamw)_\w+)\s*\(", text)))
-    assert len(names) == 15
+    assert len(names) == 14
     for n in names:
         assert ctypes.cast(getattr(L, n), ctypes.c_void_p).value
 
@@ -78,11 +78,11 @@ def test_dequantize_pack_unpack_refusals(L):
 
 
 def test_matmul_and_linear_refusals(L):
-    def mm(a=FAKE, b=FAKE, m=4, n=8, k=40, c=FAKE, type=1, ldc=8, ws=FAKE, wsb=1 << 40):
-        return L.emb_mx4_matmul(a, b, m, n, k, c, type, ldc, ws, wsb, None)
+    def mm(a=FAKE, b=FAKE, m=4, n=8, k=40, c=FAKE, type=1, ldc=8):
+        return L.emb_mx4_matmul(a, b, m, n, k, c, type, ldc, None)
 
     for bad in (dict(a=None), dict(b=None), dict(c=None), dict(a=FAKE + 4), dict(b=FAKE + 4), dict(c=FAKE + 1), dict(m=-1),
-                dict(n=-1), dict(k=-1), dict(ldc=7), dict(type=9), dict(m=2**31)):
+                dict(n=-1), dict(k=-1), dict(ldc=7), dict(type=9), dict(m=2**31), dict(k=2**24 + 1)):
         assert mm(**bad) == EINVAL, bad
     assert mm(m=0, c=None) == 0 and mm(n=0, c=None) == 0
 
@@ -95,19 +95,17 @@ def test_matmul_and_linear_refusals(L):
     assert lin(m=0, x=None, y=None) == 0
 
 
-def test_workspaces_are_checked(L):
-    """A workspace that a shape needs must be there, aligned and large enough."""
+def test_workspace_is_checked(L):
+    """The workspace that a linear layer needs must be there, aligned and large enough."""
     n = ctypes.c_size_t()
-    for name, call in (("emb_mx4_matmul_workspace", lambda ws, b: L.emb_mx4_matmul(FAKE, FAKE, 40, 64, 12800, FAKE, 1, 64, ws, b, None)),
-                       ("emb_mx4_linear_workspace", lambda ws, b: L.emb_mx4_linear(FAKE, 1, 40, 12800, 12800, FAKE, 64, FAKE, 64, ws, b, None))):
-        assert getattr(L, name)(40, 64, 12800, ctypes.byref(n)) == 0
-        if n.value:
-            assert call(None, n.value) == EINVAL
-            assert call(FAKE + 8, n.value) == EINVAL
-            assert call(FAKE, n.value - 1) == ENOMEM
-        assert getattr(L, name)(-1, 64, 128, ctypes.byref(n)) == EINVAL
-        assert getattr(L, name)(4, 64, 128, None) == EINVAL
-        assert getattr(L, name)(4, 0, 128, ctypes.byref(n)) == 0 and n.value == 0
+    call = lambda ws, b: L.emb_mx4_linear(FAKE, 1, 40, 12800, 12800, FAKE, 64, FAKE, 64, ws, b, None)  # noqa: E731
+    assert L.emb_mx4_linear_workspace(40, 64, 12800, ctypes.byref(n)) == 0 and n.value
+    assert call(None, n.value) == EINVAL
+    assert call(FAKE + 8, n.value) == EINVAL
+    assert call(FAKE, n.value - 1) == ENOMEM
+    assert L.emb_mx4_linear_workspace(-1, 64, 128, ctypes.byref(n)) == EINVAL
+    assert L.emb_mx4_linear_workspace(4, 64, 128, None) == EINVAL
+    assert L.emb_mx4_linear_workspace(4, 0, 128, ctypes.byref(n)) == 0 and n.value == 0
 
 
 def adamw_config(of=(5, 33), **kw):

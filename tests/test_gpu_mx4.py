@@ -152,7 +152,9 @@ def product_bound(a, b, dtype):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 32), (1, 4, 5), (2, 130, 70), (16, 16, 128), (17, 33, 129), (31, 64, 160), (64, 64, 512),
             (65, 200, 385), (128, 128, 640), (129, 300, 96), (256, 256, 1024), (300, 520, 1100), (513, 257, 2500),
-            (1, 1000, 4096), (3, 500, 12800), (40, 96, 12800), (1000, 40, 33), (700, 1, 300), (2048, 512, 416)]
+            (1, 1000, 4096), (3, 500, 12800), (40, 96, 12800), (1000, 40, 33), (700, 1, 300), (2048, 512, 416),
+            # tiles of 128 and 256 whole and ragged, with the last group of columns short
+            (1920, 1920, 700), (4000, 4130, 400), (4096, 4096, 512), (20, 16500, 70), (16500, 20, 600), (129, 1500, 9000)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
