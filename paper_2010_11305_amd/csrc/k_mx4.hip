@@ -16,43 +16,40 @@ __device__ __forceinline__ void store_scale(uint8_t* out, const Mx4& q, int64_t 
     for (int t = (int)(kt % kScaleTiles) + 1; t < kScaleTiles; ++t) *++p = 0;
 }
 
-// By rows: a wave takes one tile, lane 16 b + r quantises block b of row r by itself (no
-// step crosses lanes), and the wave writes the tile's 1024 bytes as they lie.
-template <int TYPE, bool STOCHASTIC>
-__global__ __launch_bounds__(256) void k_quantize_rows(const typename Elem<TYPE>::type* __restrict__ x, Mx4 q,
-                                                       int64_t ld, uint8_t* __restrict__ out, Mx4Random rnd) {
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (tile >= q.row_tiles * q.col_tiles) return;
-  const int lane = threadIdx.x & 63;
-  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
-  const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
-  const int64_t left = row < q.rows ? q.cols - col : 0;
-  Raw<TYPE, kBlock> r;
-  load_values(x + (left > 0 ? row * ld + col : 0), (int)(left < 0 ? 0 : left > kBlock ? kBlock : left), r);
-  uint32_t s;
-  const uint4 c = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
-  *reinterpret_cast<uint4*>(out + q.tile(rt, kt) + 16 * lane) = c;
-  store_scale(out, q, rt, kt, lane, s);
-}
+// A workgroup stages ROWS x COLS of x in LDS, read in whole lines, and quantises it along its rows, its columns
+// or both: a thread takes 32 values that share a scale, so no step crosses lanes, and writes its 16 bytes of
+// codes where 16 threads make 256 contiguous ones.  Along columns a wave reads a row of the stage at a
+// time, two columns a thread where the elements have 16 bits.
+template <int TYPE, bool BY_ROWS, bool BY_COLUMNS>
+struct Stage {
+  static constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
+  static constexpr int kRows = BY_COLUMNS ? kTileCols : 64;
+  static constexpr int kCols = TYPE == EMB_TYPE_FP32 && BY_COLUMNS ? 64 : 128;
+  static constexpr int kPitch = kCols + kPiece;  // 16 more bytes a row: rows start in different banks
+  // The scale bytes of four tiles along a quantised axis lie in one dword: their workgroups run on one XCD, whose
+  // L2 joins them (a square of four tiles by four, or 512 columns of rows).
+  static constexpr int kSquareRows = BY_COLUMNS ? 4 : 1;
+  static constexpr int kSquareCols = 512 / kCols;
+};
 
-// By columns, and by rows from the same pass: a workgroup stages 128 rows x 64 columns in
-// LDS; then a thread takes 32 rows of one column (a wave: 64 columns, so its reads of a
-// row are contiguous), and, for the rows, 32 columns of one row.
-constexpr int kStageRows = 128, kStageCols = 64;
-
-template <int TYPE, bool STOCHASTIC, bool ROWS>
-__global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TYPE>::type* __restrict__ x, Mx4 qr,
-                                                          Mx4 qc, int64_t ld, uint8_t* __restrict__ by_rows,
-                                                          uint8_t* __restrict__ by_columns, Mx4Random rnd) {
+template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
+__global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::type* __restrict__ x, Mx4 qr, Mx4 qc,
+                                                  int64_t ld, uint8_t* __restrict__ by_rows,
+                                                  uint8_t* __restrict__ by_columns, Mx4Random rnd) {
   using E = typename Elem<TYPE>::type;
-  constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
-  constexpr int kPitch = kStageCols + kPiece;  // 16 more bytes a row: rows start in different banks
-  __shared__ __attribute__((aligned(16))) E stage[kStageRows * kPitch];
-  const int64_t tiles_c = (qr.cols + kStageCols - 1) / kStageCols;
-  const int64_t row0 = (int64_t)blockIdx.x / tiles_c * kStageRows, col0 = (int64_t)blockIdx.x % tiles_c * kStageCols;
-  constexpr int kPieces = kStageCols / kPiece;
+  using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
+  constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = St::kCols / kPiece;
+  __shared__ __attribute__((aligned(16))) E stage[St::kRows * kPitch];
+  // workgroups go to the XCDs in turn: square n of XCD x is square 8 n + x
+  constexpr int kSquare = St::kSquareRows * St::kSquareCols;
+  const int64_t wide = (qr.cols + St::kCols * St::kSquareCols - 1) / (St::kCols * St::kSquareCols);
+  const int64_t square = (int64_t)blockIdx.x / (8 * kSquare) * 8 + blockIdx.x % 8;
+  const int in = blockIdx.x / 8 % kSquare;
+  const int64_t row0 = (square / wide * St::kSquareRows + in / St::kSquareCols) * St::kRows;
+  const int64_t col0 = (square % wide * St::kSquareCols + in % St::kSquareCols) * St::kCols;
+  if (row0 >= qr.row_tiles * kTileRows || col0 >= qr.col_tiles * kTileCols) return;
 #pragma unroll
-  for (int i = 0; i < kStageRows * kPieces / 256; ++i) {
+  for (int i = 0; i < St::kRows * kPieces / 256; ++i) {
     const int id = i * 256 + threadIdx.x, r = id / kPieces, c = id % kPieces * kPiece;
     const int64_t row = row0 + r, left = row < qr.rows ? qr.cols - col0 - c : 0;
     Raw<TYPE, kPiece> v;
@@ -60,26 +57,40 @@ __global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TY
     *reinterpret_cast<uint4*>(&stage[r * kPitch + c]) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
   }
   __syncthreads();
-  {
-    const int c = threadIdx.x & 63, b = threadIdx.x >> 6;
-    const int64_t col = col0 + c, rt = col / kTileRows, kt = row0 / kTileCols;
-    if (rt < qc.row_tiles) {
-      Raw<TYPE, kBlock> r;
+  if constexpr (BY_COLUMNS) {
+    constexpr int kPer = 4 / Elem<TYPE>::kBytes;    // columns a thread
+    const int c = threadIdx.x % 64 * kPer, b = threadIdx.x / 64;
+    const int64_t kt = row0 / kTileCols;
+    Raw<TYPE, kBlock> r[kPer];
 #pragma unroll
-      for (int j = 0; j < kBlock; ++j) r.put(j, load_bits<TYPE>(&stage[(b * kBlock + j) * kPitch + c]));
+    for (int j = 0; j < kBlock; ++j) {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(&stage[(b * kBlock + j) * kPitch + c]);
+      if constexpr (kPer == 1) {
+        r[0].put(j, v);
+      } else {
+        r[0].put(j, v & 0xFFFFu);
+        r[kPer - 1].put(j, v >> 16);
+      }
+    }
+    Mx4Random q = rnd;
+    q.tag = 1;
+#pragma unroll
+    for (int p = 0; p < kPer; ++p) {
+      const int64_t col = col0 + c + p, rt = col / kTileRows;
+      if (rt >= qc.row_tiles) continue;
       uint32_t s;
-      Mx4Random q = rnd;
-      q.tag = 1;
-      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)((row0 + b * kBlock) / 8), (uint32_t)col, q, &s);
+      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r[p], (uint32_t)((row0 + b * kBlock) / 8), (uint32_t)col, q, &s);
       const int lane = b * 16 + (int)(col % kTileRows);
       *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
       store_scale(by_columns, qc, rt, kt, lane, s);
     }
   }
-  if constexpr (ROWS) {
-    const int rr = threadIdx.x & 127, h = threadIdx.x >> 7;
-    const int64_t row = row0 + rr, rt = row / kTileRows, kt = col0 / kTileCols;
-    if (rt < qr.row_tiles) {
+  if constexpr (BY_ROWS) {
+#pragma unroll
+    for (int task = threadIdx.x; task < St::kRows * St::kCols / kBlock; task += 256) {
+      const int rr = task % St::kRows, h = task / St::kRows;
+      const int64_t row = row0 + rr, col = col0 + h * kBlock, rt = row / kTileRows, kt = col / kTileCols;
+      if (rt >= qr.row_tiles) continue;
       Raw<TYPE, kBlock> r;
 #pragma unroll
       for (int i = 0; i < kBlock / kPiece; ++i) {
@@ -87,16 +98,10 @@ __global__ __launch_bounds__(256) void k_quantize_columns(const typename Elem<TY
         r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
       }
       uint32_t s;
-      const int64_t col = col0 + h * kBlock;
       const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
       const int lane = (int)(col % kTileCols / kBlock) * 16 + (int)(row % kTileRows);
       *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * lane) = code;
       store_scale(by_rows, qr, rt, kt, lane, s);
-      // the tile's other half, where no column of x is left for a workgroup of its own
-      if (col0 + kStageCols >= qr.cols && col0 % kTileCols == 0) {
-        *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * (lane + 32)) = make_uint4(0, 0, 0, 0);
-        store_scale(by_rows, qr, rt, kt, lane + 32, 0);
-      }
     }
   }
 }
@@ -184,24 +189,25 @@ __global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ cod
   scales[row * blocks + col / kBlock] = q.base[q.scale(rt, kt, lane)];
 }
 
-template <int TYPE, bool STOCHASTIC>
-hipError_t quantize_as(const void* xv, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
-                       const Mx4Random& rnd, hipStream_t s) {
-  const auto* x = static_cast<const typename Elem<TYPE>::type*>(xv);
-  const Mx4 qr(by_rows, rows, cols), qc(by_columns, cols, rows);
-  auto* r = static_cast<uint8_t*>(by_rows);
-  auto* c = static_cast<uint8_t*>(by_columns);
-  if (!c) {
-    const int64_t tiles = qr.row_tiles * qr.col_tiles;
-    k_quantize_rows<TYPE, STOCHASTIC><<<(unsigned)((tiles + 3) / 4), 256, 0, s>>>(x, qr, ld, r, rnd);
-  } else {
-    const unsigned grid = (unsigned)(((rows + kStageRows - 1) / kStageRows) * ((cols + kStageCols - 1) / kStageCols));
-    if (r)
-      k_quantize_columns<TYPE, STOCHASTIC, true><<<grid, 256, 0, s>>>(x, qr, qc, ld, r, c, rnd);
-    else
-      k_quantize_columns<TYPE, STOCHASTIC, false><<<grid, 256, 0, s>>>(x, qr, qc, ld, r, c, rnd);
-  }
+template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
+hipError_t quantize_along(const void* x, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
+                          const Mx4Random& rnd, hipStream_t s) {
+  using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const int64_t squares = up(rows, (int64_t)St::kRows * St::kSquareRows) * up(cols, (int64_t)St::kCols * St::kSquareCols);
+  const int64_t grid = up(squares, 8) * 8 * St::kSquareRows * St::kSquareCols;
+  k_quantize<TYPE, STOCHASTIC, BY_ROWS, BY_COLUMNS><<<(unsigned)grid, 256, 0, s>>>(
+      static_cast<const typename Elem<TYPE>::type*>(x), Mx4(by_rows, rows, cols), Mx4(by_columns, cols, rows), ld,
+      static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), rnd);
   return hipGetLastError();
+}
+
+template <int TYPE, bool STOCHASTIC>
+hipError_t quantize_as(const void* x, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
+                       const Mx4Random& rnd, hipStream_t s) {
+  if (!by_columns) return quantize_along<TYPE, STOCHASTIC, true, false>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
+  if (!by_rows) return quantize_along<TYPE, STOCHASTIC, false, true>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
+  return quantize_along<TYPE, STOCHASTIC, true, true>(x, rows, cols, ld, by_rows, by_columns, rnd, s);
 }
 
 }  // namespace
