@@ -16,20 +16,23 @@ __device__ __forceinline__ void store_scale(uint8_t* out, const Mx4& q, int64_t 
     for (int t = (int)(kt % kScaleTiles) + 1; t < kScaleTiles; ++t) *++p = 0;
 }
 
-// A workgroup stages ROWS x COLS of x in LDS, read in whole lines, and quantises it along its rows, its columns
-// or both: a thread takes 32 values that share a scale, so no step crosses lanes, and writes its 16 bytes of
-// codes where 16 threads make 256 contiguous ones.  Along columns a wave reads a row of the stage at a
-// time, two columns a thread where the elements have 16 bits.
+// A workgroup stages some rows x 128 columns of x in LDS, read in whole lines, and quantises them along the
+// rows, the columns or both: a thread takes 32 values that share a scale, so no step crosses lanes, and
+// writes its 16 bytes of codes where 16 threads make 256 contiguous ones.  For both, one half of
+// the threads takes the columns (a wave reads a row of the stage at a time) and the other the rows.
 template <int TYPE, bool BY_ROWS, bool BY_COLUMNS>
 struct Stage {
   static constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
-  static constexpr int kRows = BY_COLUMNS ? kTileCols : 64;
-  static constexpr int kCols = TYPE == EMB_TYPE_FP32 && BY_COLUMNS ? 64 : 128;
-  static constexpr int kPitch = kCols + kPiece;  // 16 more bytes a row: rows start in different banks
-  // The scale bytes of four tiles along a quantised axis lie in one dword: their workgroups run on one XCD, whose
-  // L2 joins them (a square of four tiles by four, or 512 columns of rows).
-  static constexpr int kSquareRows = BY_COLUMNS ? 4 : 1;
-  static constexpr int kSquareCols = 512 / kCols;
+  static constexpr int kRows = BY_COLUMNS ? kBlock : 64;
+  static constexpr int kThreads = BY_ROWS ? 256 : 128;
+  static constexpr int kPitch = kTileCols + kPiece;  // 16 more bytes a row: rows start in different banks
+  // The scale bytes of four tiles along a quantised axis lie in one dword, and a column's codes of 128 rows in one
+  // tile: where there are many workgroups those of 512 rows (by columns) x 512 columns run on one XCD, whose
+  // L2 joins what they write.
+  static constexpr int kSquareRows = BY_COLUMNS ? 512 / kRows : 1;
+  static constexpr int kSquareCols = 4;
+  static constexpr int kSquare = kSquareRows * kSquareCols;
+  static constexpr int kSquaresFrom = 64;
 };
 
 template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
@@ -38,71 +41,56 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
                                                   uint8_t* __restrict__ by_columns, Mx4Random rnd) {
   using E = typename Elem<TYPE>::type;
   using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
-  constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = St::kCols / kPiece;
+  constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = kTileCols / kPiece;
   __shared__ __attribute__((aligned(16))) E stage[St::kRows * kPitch];
-  // workgroups go to the XCDs in turn: square n of XCD x is square 8 n + x
-  constexpr int kSquare = St::kSquareRows * St::kSquareCols;
-  const int64_t wide = (qr.cols + St::kCols * St::kSquareCols - 1) / (St::kCols * St::kSquareCols);
-  const int64_t square = (int64_t)blockIdx.x / (8 * kSquare) * 8 + blockIdx.x % 8;
-  const int in = blockIdx.x / 8 % kSquare;
+  const int64_t wide = (qr.cols + kTileCols * St::kSquareCols - 1) / (kTileCols * St::kSquareCols);
+  int64_t square = blockIdx.x / St::kSquare;
+  int in = blockIdx.x % St::kSquare;
+  if (gridDim.x >= St::kSquaresFrom * St::kSquare) {  // workgroups go to the XCDs in turn
+    square = (int64_t)blockIdx.x / (8 * St::kSquare) * 8 + blockIdx.x % 8;
+    in = blockIdx.x / 8 % St::kSquare;
+  }
   const int64_t row0 = (square / wide * St::kSquareRows + in / St::kSquareCols) * St::kRows;
-  const int64_t col0 = (square % wide * St::kSquareCols + in % St::kSquareCols) * St::kCols;
-  if (row0 >= qr.row_tiles * kTileRows || col0 >= qr.col_tiles * kTileCols) return;
+  const int64_t kt0 = square % wide * St::kSquareCols + in % St::kSquareCols, col0 = kt0 * kTileCols;
+  // by columns the rows go on to the end of their tile of 128
+  const int64_t row_end = BY_COLUMNS ? qc.col_tiles * kTileCols : qr.row_tiles * kTileRows;
+  if (row0 >= row_end || kt0 >= qr.col_tiles) return;
 #pragma unroll
-  for (int i = 0; i < St::kRows * kPieces / 256; ++i) {
-    const int id = i * 256 + threadIdx.x, r = id / kPieces, c = id % kPieces * kPiece;
+  for (int i = 0; i < St::kRows * kPieces / St::kThreads; ++i) {
+    const int id = i * St::kThreads + threadIdx.x, r = id / kPieces, c = id % kPieces * kPiece;
     const int64_t row = row0 + r, left = row < qr.rows ? qr.cols - col0 - c : 0;
     Raw<TYPE, kPiece> v;
     load_values(x + (left > 0 ? row * ld + col0 + c : 0), (int)(left < 0 ? 0 : left > kPiece ? kPiece : left), v);
     *reinterpret_cast<uint4*>(&stage[r * kPitch + c]) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
   }
   __syncthreads();
-  if constexpr (BY_COLUMNS) {
-    constexpr int kPer = 4 / Elem<TYPE>::kBytes;    // columns a thread
-    const int c = threadIdx.x % 64 * kPer, b = threadIdx.x / 64;
-    const int64_t kt = row0 / kTileCols;
-    Raw<TYPE, kBlock> r[kPer];
+  Raw<TYPE, kBlock> r;
+  uint32_t s;
+  if (BY_COLUMNS && threadIdx.x < 128) {
+    const int c = threadIdx.x;
+    const int64_t col = col0 + c, rt = col / kTileRows, kt = row0 / kTileCols;
+    if (rt >= qc.row_tiles) return;
 #pragma unroll
-    for (int j = 0; j < kBlock; ++j) {
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(&stage[(b * kBlock + j) * kPitch + c]);
-      if constexpr (kPer == 1) {
-        r[0].put(j, v);
-      } else {
-        r[0].put(j, v & 0xFFFFu);
-        r[kPer - 1].put(j, v >> 16);
-      }
-    }
+    for (int j = 0; j < kBlock; ++j) r.put(j, load_bits<TYPE>(&stage[j * kPitch + c]));
     Mx4Random q = rnd;
     q.tag = 1;
+    const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(row0 / 8), (uint32_t)col, q, &s);
+    const int lane = (int)(row0 % kTileCols / kBlock) * 16 + (int)(col % kTileRows);
+    *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
+    store_scale(by_columns, qc, rt, kt, lane, s);
+  } else if constexpr (BY_ROWS) {
+    const int task = threadIdx.x - (BY_COLUMNS ? 128 : 0), rr = task % St::kRows, h = task / St::kRows;
+    const int64_t row = row0 + rr, col = col0 + h * kBlock, rt = row / kTileRows;
+    if (rt >= qr.row_tiles) return;
 #pragma unroll
-    for (int p = 0; p < kPer; ++p) {
-      const int64_t col = col0 + c + p, rt = col / kTileRows;
-      if (rt >= qc.row_tiles) continue;
-      uint32_t s;
-      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r[p], (uint32_t)((row0 + b * kBlock) / 8), (uint32_t)col, q, &s);
-      const int lane = b * 16 + (int)(col % kTileRows);
-      *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
-      store_scale(by_columns, qc, rt, kt, lane, s);
+    for (int i = 0; i < kBlock / kPiece; ++i) {
+      const uint4 v = *reinterpret_cast<const uint4*>(&stage[rr * kPitch + h * kBlock + i * kPiece]);
+      r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
     }
-  }
-  if constexpr (BY_ROWS) {
-#pragma unroll
-    for (int task = threadIdx.x; task < St::kRows * St::kCols / kBlock; task += 256) {
-      const int rr = task % St::kRows, h = task / St::kRows;
-      const int64_t row = row0 + rr, col = col0 + h * kBlock, rt = row / kTileRows, kt = col / kTileCols;
-      if (rt >= qr.row_tiles) continue;
-      Raw<TYPE, kBlock> r;
-#pragma unroll
-      for (int i = 0; i < kBlock / kPiece; ++i) {
-        const uint4 v = *reinterpret_cast<const uint4*>(&stage[rr * kPitch + h * kBlock + i * kPiece]);
-        r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
-      }
-      uint32_t s;
-      const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
-      const int lane = (int)(col % kTileCols / kBlock) * 16 + (int)(row % kTileRows);
-      *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt) + 16 * lane) = code;
-      store_scale(by_rows, qr, rt, kt, lane, s);
-    }
+    const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(col / 8), (uint32_t)row, rnd, &s);
+    const int lane = h * 16 + (int)(row % kTileRows);
+    *reinterpret_cast<uint4*>(by_rows + qr.tile(rt, kt0) + 16 * lane) = code;
+    store_scale(by_rows, qr, rt, kt0, lane, s);
   }
 }
 
@@ -194,9 +182,9 @@ hipError_t quantize_along(const void* x, int64_t rows, int64_t cols, int64_t ld,
                           const Mx4Random& rnd, hipStream_t s) {
   using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  const int64_t squares = up(rows, (int64_t)St::kRows * St::kSquareRows) * up(cols, (int64_t)St::kCols * St::kSquareCols);
-  const int64_t grid = up(squares, 8) * 8 * St::kSquareRows * St::kSquareCols;
-  k_quantize<TYPE, STOCHASTIC, BY_ROWS, BY_COLUMNS><<<(unsigned)grid, 256, 0, s>>>(
+  const int64_t squares = up(rows, St::kRows * St::kSquareRows) * up(cols, kTileCols * St::kSquareCols);
+  const int64_t grid = (squares >= St::kSquaresFrom ? up(squares, 8) * 8 : squares) * St::kSquare;
+  k_quantize<TYPE, STOCHASTIC, BY_ROWS, BY_COLUMNS><<<(unsigned)grid, St::kThreads, 0, s>>>(
       static_cast<const typename Elem<TYPE>::type*>(x), Mx4(by_rows, rows, cols), Mx4(by_columns, cols, rows), ld,
       static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), rnd);
   return hipGetLastError();
