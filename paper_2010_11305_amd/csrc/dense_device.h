@@ -138,6 +138,19 @@ __device__ __forceinline__ uint32_t mx4_scale(uint32_t amax) {
   return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
 }
 
+// embc::philox4x32_10 with the three-way exclusive or as one instruction.
+__device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c.x, p1 = (uint64_t)0xCD9E8D57u * c.z;
+    c = make_uint4(__builtin_amdgcn_bitop3_b32((uint32_t)(p1 >> 32), c.y, k0, 0x96), (uint32_t)p1,
+                   __builtin_amdgcn_bitop3_b32((uint32_t)(p0 >> 32), c.w, k1, 0x96), (uint32_t)p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return c;
+}
+
 // Where a block lies in the random stream: key, and the counter of its first 8 values.
 struct Mx4Random {
   uint32_t k0, k1, step, tag;
@@ -171,7 +184,7 @@ __device__ __forceinline__ uint32_t codes8_nearest(const Raw<TYPE, N>& r, int j0
 template <int TYPE, int N>
 __device__ __forceinline__ uint32_t codes8_stochastic(const Raw<TYPE, N>& r, int j0, uint32_t scale, uint32_t col8,
                                                       uint32_t row, const Mx4Random& q) {
-  const uint4 w = embc::philox4x32_10(make_uint4(col8, row, q.step, q.tag), q.k0, q.k1);
+  const uint4 w = philox(make_uint4(col8, row, q.step, q.tag), q.k0, q.k1);
   const uint32_t rest[4] = {~w.x, ~w.y, ~w.z, ~w.w};   // 2^16 - 1 - u, two a word
   const int up = 150 - (int)scale;
   uint32_t c[8];

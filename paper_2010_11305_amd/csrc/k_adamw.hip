@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamDev d, AdamPointers ptr, uint
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint64_t n4 = (uint64_t)(at / 4 + h);
-        const uint4 w = embc::philox4x32_10(make_uint4((uint32_t)n4, (uint32_t)(n4 >> 32), c.t, 0), c.k0, c.k1);
+        const uint4 w = philox(make_uint4((uint32_t)n4, (uint32_t)(n4 >> 32), c.t, 0), c.k0, c.k1);
         word[4 * h] = w.x, word[4 * h + 1] = w.y, word[4 * h + 2] = w.z, word[4 * h + 3] = w.w;
       }
     }
