@@ -138,6 +138,61 @@ def test_steps(torch, param, grad, bits, rounding):
     assert (flat.cpu()[keep] == 7.0).all()
 
 
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", ["float32", "bfloat16"])
+def test_bits_of_one_step(torch, param, bits, rounding):
+    """The step is defined operation by operation in FP32, and its roundings by given bits: numpy's FP32 operations
+    (IEEE, as the kernel's) and the grids give every stored bit."""
+    from paper_2010_11305_amd.adamw import AdamW
+
+    n, t, seed = 5003, 8, 1234
+    _, (p,) = tensors(torch, [n], getattr(torch, param), 5, 0.05)
+    _, (g,) = tensors(torch, [n], torch.float32, 6, 1e-2)
+    g[::7] = 0.0
+    opt = AdamW([p], lr=LR, betas=(B1, B2), eps=EPS, weight_decay=0.1, grad_dtype=torch.float32, state_bits=bits,
+                rounding=rounding, seed=seed)
+    for _ in range(t - 1):
+        opt.step([g])
+        g = g.flip(0).contiguous()
+    m, v = (x[:n].astype(np.float32) for x in second(opt.state(), bits))
+    if bits == 8:      # v is the square of the root that is kept, in FP32
+        r = np.sqrt(second(opt.state(), 8)[1][:n]).astype(np.float32)
+        v = r * r
+    before, grad = p.float().cpu().numpy(), g.cpu().numpy()
+    opt.step([g])
+    f = np.float32
+    m = m * f(B1) + grad * f(1 - B1)
+    v = v * f(B2) + (grad * grad) * f(1 - B2)
+    root = np.sqrt(v)
+    want = before * f(1 - LR * 0.1) - (m / (root * f(1 / np.sqrt(1 - B2**t)) + f(EPS))) * f(LR / (1 - B1**t))
+    um, ur, up = ref.adam_random_bits(np.arange(n), t, seed)
+    if param == "bfloat16":
+        b = want.view(np.uint32).astype(np.uint64)
+        if rounding == "stochastic":
+            b = (b + up.astype(np.uint64)) >> np.uint64(16)
+            assert np.array_equal(p.view(torch.int16).cpu().numpy().view(np.uint16), b.astype(np.uint16))
+        else:
+            assert torch.equal(p.cpu(), torch.from_numpy(want).bfloat16())
+    else:
+        assert np.array_equal(p.cpu().numpy().view(np.uint32), want.view(np.uint32))
+    state = {k: x.view(torch.uint8).cpu().numpy() for k, x in opt.state().items()}
+    if bits == 32:
+        assert np.array_equal(state["exp_avg"].view(np.float32)[:n], m)
+        assert np.array_equal(state["exp_avg_sq"].view(np.float32)[:n], v)
+        return
+    for name, x, u in (("exp_avg", m, um), ("exp_avg_root", root, ur)):
+        block = np.zeros(-(-n // 32) * 32)
+        block[:n] = np.abs(x)
+        s = ref.e4m3_scale(block.reshape(-1, 32).max(1))
+        assert np.array_equal(state[name + "_scale"], s)
+        y = np.abs(x.astype(np.float64)) / np.repeat(np.exp2(s - 127.0), 32)[:n]
+        code = ref.on_grid(y, ref.GRID8, u if rounding == "stochastic" else None)
+        if name == "exp_avg_root":
+            code = np.where(x > 0, np.maximum(code, 1), code)
+        assert np.array_equal(state[name][:n], code + 128 * np.signbit(x))
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_many_tensors(torch, bits):
     """More tensors than one launch carries, each as if it were alone (rounding to nearest: no draw by place)."""
