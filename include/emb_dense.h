@@ -86,6 +86,30 @@ int emb_mx4_linear_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
 int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                    int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
+/* One training pass of the layer, in two calls that only put the ones above together.
+ *
+ * emb_mx4_linear_train: y [m][n] = Q(x) w^T with w by rows, and `saved`, the MX4 matrix [k][m] of
+ * the transpose of x that the backward pass needs (emb_mx4_query_bytes(k, m)); x rounds as
+ * `rounding` says (seed and step when stochastic).  y in the type of x.
+ *
+ * emb_mx4_linear_grad: for an output gradient dy [m][n], rounded as `rounding` says,
+ *   dx [m][k] = Q(dy) Q(w^T)^T   in the type of dy, w_columns the MX4 matrix [k][n] of w^T
+ *   dw [n][k] = Q(dy^T) saved^T  in dw_type
+ * The rounding of the codes is the gradients' only approximation: as usual they are those
+ * of the unrounded layer, taken at the rounded values.
+ *
+ * workspace: the bytes that the function's own query reports, 256-byte aligned, or NULL when
+ * that is 0.  Enqueue-only. */
+int emb_mx4_linear_train_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
+int emb_mx4_linear_train(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n,
+                         void* y, int64_t ldy, void* saved, int32_t rounding, uint64_t seed, uint32_t step,
+                         void* workspace, size_t workspace_bytes, void* stream);
+int emb_mx4_linear_grad_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
+int emb_mx4_linear_grad(const void* dy, int32_t type, int64_t m, int64_t n, int64_t ldy, const void* w_columns, int64_t k,
+                        const void* saved, void* dx, int64_t ldx, void* dw, int32_t dw_type, int64_t ldw,
+                        int32_t rounding, uint64_t seed, uint32_t step, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
 /* AdamW over `num_tensors` tensors.  Per element, in FP32 with one rounding per
  * operation, t = steps done including this one:
  *   g = gradient * *grad_scale

@@ -161,6 +161,47 @@ int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ld
   return status(launch_linear(x, type, m, k, ldx, w, n, y, ldy, workspace, S(stream)));
 }
 
+int emb_mx4_linear_train_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
+  if (!bytes || !product_ok(m, n, k) || !dims_ok(k, m)) return EMB_EINVAL;
+  *bytes = m && k ? (size_t)Mx4(nullptr, m, k).bytes() : 0;
+  return EMB_OK;
+}
+
+int emb_mx4_linear_train(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n,
+                         void* y, int64_t ldy, void* saved, int32_t rounding, uint64_t seed, uint32_t step,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  if (emb_mx4_linear_train_workspace(m, n, k, &need) != EMB_OK) return EMB_EINVAL;
+  if (need && (!workspace || !aligned(workspace) || !saved)) return EMB_EINVAL;
+  if (m && n && (!type_ok(type) || !matrix_ok(y, type, m, n, ldy) || (k && (!w || !aligned(w))))) return EMB_EINVAL;
+  if (workspace_bytes < need) return EMB_ENOMEM;
+  const int st = emb_mx4_quantize(x, type, m, k, ldx, workspace, saved, rounding, seed, step, stream);
+  return st != EMB_OK ? st : emb_mx4_matmul(workspace, w, m, n, k, y, type, ldy, stream);
+}
+
+int emb_mx4_linear_grad_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
+  if (!bytes || !product_ok(m, k, n) || !product_ok(n, k, m)) return EMB_EINVAL;
+  *bytes = m && n ? align_up((size_t)Mx4(nullptr, m, n).bytes()) + (size_t)Mx4(nullptr, n, m).bytes() : 0;
+  return EMB_OK;
+}
+
+int emb_mx4_linear_grad(const void* dy, int32_t type, int64_t m, int64_t n, int64_t ldy, const void* w_columns, int64_t k,
+                        const void* saved, void* dx, int64_t ldx, void* dw, int32_t dw_type, int64_t ldw,
+                        int32_t rounding, uint64_t seed, uint32_t step, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+  size_t need = 0;
+  if (emb_mx4_linear_grad_workspace(m, n, k, &need) != EMB_OK || !type_ok(type) || !type_ok(dw_type)) return EMB_EINVAL;
+  if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
+  if (m && k && (!matrix_ok(dx, type, m, k, ldx) || (n && (!w_columns || !aligned(w_columns))))) return EMB_EINVAL;
+  if (n && k && (!matrix_ok(dw, dw_type, n, k, ldw) || (m && (!saved || !aligned(saved))))) return EMB_EINVAL;
+  if (workspace_bytes < need) return EMB_ENOMEM;
+  uint8_t* rows = static_cast<uint8_t*>(workspace);
+  uint8_t* columns = need ? rows + align_up((size_t)Mx4(nullptr, m, n).bytes()) : nullptr;
+  int st = emb_mx4_quantize(dy, type, m, n, ldy, rows, columns, rounding, seed, step, stream);
+  if (st == EMB_OK) st = emb_mx4_matmul(rows, w_columns, m, k, n, dx, type, ldx, stream);
+  return st != EMB_OK ? st : emb_mx4_matmul(columns, saved, n, k, m, dw, dw_type, ldw, stream);
+}
+
 int emb_adamw_query_sizes(const emb_adamw_config* cfg, emb_adamw_sizes* out) {
   if (!out) return EMB_EINVAL;
   try {

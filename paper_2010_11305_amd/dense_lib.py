@@ -60,6 +60,10 @@ def load():
         "emb_mx4_matmul": [P, P, i64, i64, i64, P, i32, i64, P],
         "emb_mx4_linear_workspace": [i64, i64, i64, c.POINTER(size)],
         "emb_mx4_linear": [P, i32, i64, i64, i64, P, i64, P, i64, P, size, P],
+        "emb_mx4_linear_train_workspace": [i64, i64, i64, c.POINTER(size)],
+        "emb_mx4_linear_train": [P, i32, i64, i64, i64, P, i64, P, i64, P, i32, u64, u32, P, size, P],
+        "emb_mx4_linear_grad_workspace": [i64, i64, i64, c.POINTER(size)],
+        "emb_mx4_linear_grad": [P, i32, i64, i64, i64, P, i64, P, P, i64, P, i32, i64, i32, u64, u32, P, size, P],
         "emb_adamw_query_sizes": [c.POINTER(AdamwConfig), c.POINTER(AdamwSizes)],
         "emb_adamw_create": [c.POINTER(AdamwConfig), P, size, P, c.POINTER(P)],
         "emb_adamw_destroy": [P],

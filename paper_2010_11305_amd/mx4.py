@@ -185,10 +185,29 @@ class Linear:
 
     def forward_train(self, x, step=0):
         """(y, what backward needs of x: its 4-bit form along the batch)."""
-        rows, saved = quantize_both(x, self.rounding, self.seed, step)
-        return matmul(rows, self.by_rows, x.dtype), saved
+        p, t, m, k, ld = lib.matrix(x, "x")
+        n, dev = self.out_features, x.device
+        if k != self.in_features or dev != self.by_rows.device:
+            raise ValueError(f"x must be [rows, {self.in_features}] on {self.by_rows.device}")
+        saved = Mx4Matrix(k, m, dev)
+        y = torch.empty((m, n), dtype=x.dtype, device=dev)
+        need = _query("emb_mx4_linear_train_workspace", m, n, k)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        lib.call("emb_mx4_linear_train", dev, p, t, m, k, ld, self.by_rows.data.data_ptr(), n, y.data_ptr(), max(n, 1),
+                 saved.data.data_ptr(), lib.rounding_of(self.rounding), self.seed, step, ws.data_ptr(), need)
+        return y, saved
 
     def backward(self, dy, saved: Mx4Matrix, step=0, weight_grad_dtype=torch.float32):
         """(dx in the type of dy, dw [out_features, in_features])."""
-        rows, cols = quantize_both(dy, self.grad_rounding, self.seed, step)
-        return matmul(rows, self.by_columns, dy.dtype), matmul(cols, saved, weight_grad_dtype)
+        p, t, m, n, ld = lib.matrix(dy, "dy")
+        k, dev = self.in_features, dy.device
+        if n != self.out_features or saved.shape != (k, m) or dev != self.by_rows.device or saved.device != dev:
+            raise ValueError(f"dy must be [rows, {self.out_features}] and saved [{k}, rows], on {self.by_rows.device}")
+        dx = torch.empty((m, k), dtype=dy.dtype, device=dev)
+        dw = torch.empty((n, k), dtype=weight_grad_dtype, device=dev)
+        need = _query("emb_mx4_linear_grad_workspace", m, n, k)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        lib.call("emb_mx4_linear_grad", dev, p, t, m, n, ld, self.by_columns.data.data_ptr(), k, saved.data.data_ptr(),
+                 dx.data_ptr(), max(k, 1), dw.data_ptr(), lib.type_of(weight_grad_dtype), max(k, 1),
+                 lib.rounding_of(self.grad_rounding), self.seed, step, ws.data_ptr(), need)
+        return dx, dw

@@ -28,7 +28,7 @@ def L():
 def test_every_declared_symbol_is_exported(L):
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "emb_dense.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(emb_(?:mx4|adamw)_\w+)\s*\(", text)))
-    assert len(names) == 14
+    assert len(names) == 18
     for n in names:
         assert ctypes.cast(getattr(L, n), ctypes.c_void_p).value
 
@@ -93,6 +93,33 @@ def test_matmul_and_linear_refusals(L):
                 dict(ldx=39), dict(ldy=7), dict(type=7), dict(n=2**31)):
         assert lin(**bad) == EINVAL, bad
     assert lin(m=0, x=None, y=None) == 0
+
+
+def test_training_call_refusals(L):
+    n = ctypes.c_size_t()
+    assert L.emb_mx4_linear_train_workspace(40, 64, 128, ctypes.byref(n)) == 0 and n.value == 3 * 1024 + 3 * 256
+    assert L.emb_mx4_linear_train_workspace(0, 64, 128, ctypes.byref(n)) == 0 and n.value == 0
+    assert L.emb_mx4_linear_grad_workspace(40, 64, 128, ctypes.byref(n)) == 0 and n.value == (3 + 4) * 1280
+
+    def train(x=FAKE, type=1, m=40, k=128, ldx=128, w=FAKE, n=64, y=FAKE, ldy=64, saved=FAKE, rounding=0, ws=FAKE,
+              wsb=1 << 30):
+        return L.emb_mx4_linear_train(x, type, m, k, ldx, w, n, y, ldy, saved, rounding, 0, 0, ws, wsb, None)
+
+    for bad in (dict(x=None), dict(x=FAKE + 1), dict(type=3), dict(m=-1), dict(k=-1), dict(ldx=127), dict(w=None), dict(w=FAKE + 8),
+                dict(y=None), dict(ldy=63), dict(saved=None), dict(saved=FAKE + 8), dict(rounding=3), dict(ws=None),
+                dict(ws=FAKE + 8), dict(k=2**24 + 1)):
+        assert train(**bad) == EINVAL, bad
+    assert train(wsb=3839) == ENOMEM
+
+    def grad(dy=FAKE, type=1, m=40, n=64, ldy=64, w=FAKE, k=128, saved=FAKE, dx=FAKE, ldx=128, dw=FAKE, dwt=0, ldw=128,
+             rounding=1, ws=FAKE, wsb=1 << 30):
+        return L.emb_mx4_linear_grad(dy, type, m, n, ldy, w, k, saved, dx, ldx, dw, dwt, ldw, rounding, 0, 0, ws, wsb, None)
+
+    for bad in (dict(dy=None), dict(type=3), dict(m=-1), dict(n=-1), dict(ldy=63), dict(w=None), dict(w=FAKE + 8), dict(saved=None),
+                dict(saved=FAKE + 8), dict(dx=None), dict(ldx=127), dict(dw=None), dict(dwt=3), dict(dw=FAKE + 2), dict(ldw=127),
+                dict(rounding=3), dict(ws=None), dict(ws=FAKE + 8), dict(m=2**24 + 1)):
+        assert grad(**bad) == EINVAL, bad
+    assert grad(wsb=7 * 1280 - 1) == ENOMEM
 
 
 def test_workspace_is_checked(L):

@@ -137,6 +137,13 @@ def test_empty_matrices(torch):
         x = torch.empty(rows, cols, device="cuda")
         r, c = mx4.quantize_both(x)
         assert r.shape == (rows, cols) and c.shape == (cols, rows) and r.dequantize().shape == (rows, cols)
+    for m, n, k in ((0, 4, 5), (3, 0, 5), (3, 4, 0)):
+        layer = mx4.Linear(n, k)
+        layer.load(torch.ones(n, k, device="cuda"))
+        y, saved = layer.forward_train(torch.ones(m, k, device="cuda"))
+        dx, dw = layer.backward(torch.ones(m, n, device="cuda"), saved)
+        for t, shape in ((y, (m, n)), (dx, (m, k)), (dw, (n, k))):
+            assert t.shape == shape and (t == 0).all()
     a, b = mx4.quantize(torch.empty(3, 0, device="cuda")), mx4.quantize(torch.empty(4, 0, device="cuda"))
     out = torch.full((3, 6), 2.0, device="cuda")
     mx4.matmul(a, b, out=out[:, :4])
