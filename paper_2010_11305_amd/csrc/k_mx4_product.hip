@@ -41,6 +41,14 @@ __device__ __forceinline__ void mma_done() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// An accumulator on its way out, kept where it is until here: the compiler would copy all 256 registers at once for two
+// ways of storing them, and spill (FP32, 4096x4096x8192: 80 us, without 65).
+template <int FM>
+__device__ __forceinline__ f32x4 fetched(f32x4 v) {
+  if constexpr (FM == 8) asm volatile("" : "+a"(v));
+  return v;
+}
+
 // The rows of C are the columns of an instruction's result (b is its first operand), so that a
 // lane holds four consecutive columns of a row of C.
 
@@ -106,103 +114,121 @@ __device__ __forceinline__ void stage_ready() {
 
 constexpr int kStages = 4;  // one per tile column of a scale group: the loop's body is four steps
 
-// A workgroup of 2 x 2 waves computes (32 FM) x (32 FN) of C, a wave FM x FN tiles of 16 x 16.
-template <int TYPE, int FM, int FN>
+// Tiles of 256 x 256 leave one workgroup to a CU (accumulators fill half its registers, four stages its LDS), so
+// nothing would run beside the end of a tile and the start of the next: there a workgroup stays and takes
+// tile after tile, and the last steps of one load the first stages of the next.
+template <int FM>
+constexpr bool kStays = FM == 8;
+constexpr int kResident = 256;   // workgroups that stay: one to a CU
+
+// A workgroup of 2 x 2 waves computes (32 FM) x (32 FM) of C, a wave FM x FM tiles of 16 x 16.
+template <int TYPE, int FM>
 __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
                                                                  typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
-  static_assert(FM == FN, "a wave loads tiles of one operand");
-  constexpr int kTiles = 2 * FM + 2 * FN;       // of a stage
-  constexpr int kLoads = kTiles / 4;            // a wave's share of them
+  constexpr int kSide = 2 * FM;                       // row tiles of an operand in a stage
+  constexpr int kTiles = 2 * kSide;
+  constexpr int kLoads = kTiles / 4;                  // a wave's share of them, all of one operand
   constexpr int kScaleLoads = FM >= 4 ? FM / 4 : 1;   // 4 row tiles each
+  // Results leave 16 rows x 256 bytes (or a wave's whole width) at a time, through 4 KB of LDS for each wave: beside
+  // the stages where the next tile's are in them, else over them.
+  constexpr int kBytes = Elem<TYPE>::kBytes;
+  constexpr int kOutCols = FM * 16 * kBytes <= 256 ? FM * 16 : 256 / kBytes;
+  constexpr int kLanes = kOutCols * kBytes / 16, kRows = 64 / kLanes;   // lanes a row, rows an access
   __shared__ v4i stage[kStages][kTiles][64];
   __shared__ uint32_t scales[2][kTiles][64];
+  __shared__ v4i leave[kStays<FM> ? 4 : 1][kStays<FM> ? 256 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
   // Workgroups go to the XCDs in turn.  Each XCD takes a run of consecutive tiles, in bands of 8 tile rows, so that what
   // its L2 holds is used by the workgroups that run there together.
-  const int64_t mt_all = (a.row_tiles + 2 * FM - 1) / (2 * FM), nt_all = (b.row_tiles + 2 * FN - 1) / (2 * FN);
-  const int64_t total = mt_all * nt_all;
-  const int64_t per = total / 8, more = total % 8, xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
-  const int64_t id = xcd * per + (xcd < more ? xcd : more) + nth;
-  const int64_t band = id / (8 * nt_all), in_band = id % (8 * nt_all);
-  const int64_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
-  const int64_t mt = band * 8 + in_band % band_rows, nt = in_band / band_rows;
-  const int64_t rt_a = mt * 2 * FM, rt_b = nt * 2 * FN;
+  const int64_t mt_all = (a.row_tiles + kSide - 1) / kSide, nt_all = (b.row_tiles + kSide - 1) / kSide;
+  const int64_t total = mt_all * nt_all, xcd = blockIdx.x % 8;
+  const int64_t run0 = xcd * (total / 8) + (xcd < total % 8 ? xcd : total % 8);
+  const int64_t run = total / 8 + (xcd < total % 8 ? 1 : 0);
+  const int64_t stride = (gridDim.x + 7) / 8;
+  const auto place = [&](int64_t nth, int64_t* rt_a, int64_t* rt_b) {
+    const int64_t id = run0 + nth, band = id / (8 * nt_all), in_band = id % (8 * nt_all);
+    const int64_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
+    *rt_a = (band * 8 + in_band % band_rows) * kSide;
+    *rt_b = in_band / band_rows * kSide;
+  };
 
   const int KT = (int)a.col_tiles, KG = (int)a.col_groups;
   const bool of_a = wave < 2;
   const Mx4& mine = of_a ? a : b;
-  // Row tiles past the last one are read from it: their products are not stored.
-  const auto row_tile = [&](int64_t rt) { return rt < mine.row_tiles ? rt : mine.row_tiles - 1; };
-  const int64_t rt0 = row_tile((of_a ? rt_a : rt_b) + (wave & 1) * kLoads);   // first row tile that this wave loads
-  const Srd codes = make_srd(mine.base + mine.tile(rt0, 0));
-  uint32_t code_at[kLoads];
+  // What this wave loads: row tiles past the last one are read from it, their products are not stored.
+  Srd codes, scale_srd;
+  uint32_t code_at[kLoads], scale_at[kScaleLoads];   // a scale load is of 4 row tiles, 16 lanes each
+  const auto aim = [&](int64_t rt_a, int64_t rt_b) {
+    const auto row_tile = [&](int64_t rt) { return rt < mine.row_tiles ? rt : mine.row_tiles - 1; };
+    const int64_t rt0 = row_tile((of_a ? rt_a : rt_b) + (wave & 1) * kLoads);
+    codes = make_srd(mine.base + mine.tile(rt0, 0));
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) code_at[i] = (uint32_t)(row_tile(rt0 + i) - rt0) * (uint32_t)KT * kTileBytes + lane * 16;
-  const int64_t rs0 = row_tile((of_a ? rt_a : rt_b) + (FM >= 4 ? (wave & 1) * FM : 0));
-  const Srd scale_srd = make_srd(mine.base + mine.scale_offset + rs0 * KG * kScaleBytes);
-  uint32_t scale_at[kScaleLoads];   // 4 row tiles a load, 16 lanes each
+    for (int i = 0; i < kLoads; ++i) code_at[i] = (uint32_t)(row_tile(rt0 + i) - rt0) * (uint32_t)KT * kTileBytes + lane * 16;
+    const int64_t rs0 = row_tile((of_a ? rt_a : rt_b) + (FM >= 4 ? (wave & 1) * FM : 0));
+    scale_srd = make_srd(mine.base + mine.scale_offset + rs0 * KG * kScaleBytes);
 #pragma unroll
-  for (int i = 0; i < kScaleLoads; ++i)
-    scale_at[i] = (uint32_t)(row_tile(rs0 + 4 * i + (lane >> 4)) - rs0) * (uint32_t)KG * kScaleBytes + (lane & 15) * 16;
+    for (int i = 0; i < kScaleLoads; ++i)
+      scale_at[i] = (uint32_t)(row_tile(rs0 + 4 * i + (lane >> 4)) - rs0) * (uint32_t)KG * kScaleBytes + (lane & 15) * 16;
+  };
   const uint32_t stage_at = lds_address(&stage[0][wave * kLoads][0]);
-  const uint32_t scales_at = lds_address(&scales[0][(of_a ? 0 : 2 * FM) + (FM >= 4 ? (wave & 1) * FM : 0)][0]);
+  const uint32_t scales_at = lds_address(&scales[0][(of_a ? 0 : kSide) + (FM >= 4 ? (wave & 1) * FM : 0)][0]);
 
   // Column tiles past the last one are loaded from it again, so that the number of loads in flight
   // stays the same; the steps of the last group that run over them have scale bytes 0 on both
   // sides, 2^-254 of whatever finite codes are there, which FP32 sums do not see.
-  const auto load_part = [&](int kt, int i) {
+  const auto load_part = [&](int s, int kt, int i) {
     const int k = kt < KT ? kt : KT - 1;
-    load_to_lds(stage_at + (kt % kStages) * (kTiles * 1024) + i * 1024, code_at[i], codes, k * kTileBytes);
+    load_to_lds(stage_at + s * (kTiles * 1024) + i * 1024, code_at[i], codes, k * kTileBytes);
   };
-  const auto load_stage = [&](int kt) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_part(kt, i);
-  };
-  const auto load_scales = [&](int kg) {
+  const auto load_scales = [&](int parity, int kg) {
     const int k = kg < KG ? kg : KG - 1;
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i)
-      load_to_lds(scales_at + (kg % 2) * (kTiles * 256) + i * 1024, scale_at[i], scale_srd, k * kScaleBytes);
+      load_to_lds(scales_at + parity * (kTiles * 256) + i * 1024, scale_at[i], scale_srd, k * kScaleBytes);
   };
 
-  f32x4 acc[FM][FN] = {};
-  v4i fa[2][FM], fb[2][FN];
-  uint32_t sa[FM], sb[FN], sna[FM], snb[FN];
-  load_scales(0);
-  load_stage(0);
-  load_stage(1);
-  load_stage(2);
-  load_stage(3);
+  int64_t nth = blockIdx.x / 8, rt_a, rt_b;
+  place(nth, &rt_a, &rt_b);
+  aim(rt_a, rt_b);
+  f32x4 acc[FM][FM] = {};
+  v4i fa[2][FM], fb[2][FM];
+  uint32_t sa[FM], sb[FM], sna[FM], snb[FM];
+  load_scales(0, 0);
+#pragma unroll
+  for (int s = 0; s < kStages; ++s)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_part(s, s, i);
   stage_ready<3 * kLoads>();
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     fa[0][i] = stage[0][wm * FM + i][lane], sa[i] = scales[0][wm * FM + i][lane];
-    fb[0][i] = stage[0][2 * FM + wn * FN + i][lane], sb[i] = scales[0][2 * FM + wn * FN + i][lane];
+    fb[0][i] = stage[0][kSide + wn * FM + i][lane], sb[i] = scales[0][kSide + wn * FM + i][lane];
   }
 
-  // Step kt: wait for stage kt + 1, let stage kt + 4 be loaded over stage kt (in registers since
-  // the step before), read stage kt + 1 while the products of stage kt run.  The loads and
-  // reads are spread over the products, a row of FN of them at a time: left alone, the
-  // compiler puts the reads behind them all, and the next step waits for LDS.
-  const auto step = [&](auto S, int kt) {
+  // Step s of a group: wait for the stage of the step behind it, let column tile `ahead` + s be loaded over
+  // this step's stage (in registers since the step before), read the next stage while this one's products
+  // run.  The loads and reads are spread over the products, one between two of them: left
+  // alone, the compiler puts the reads behind them all, and the next step waits for LDS.
+  int parity = 0;   // of the group's scales
+  const auto step = [&](auto S, int ahead) {
     constexpr int s = decltype(S)::value, cur = s & 1, nxt = cur ^ 1;
-    // in flight behind stage kt + 1: two later stages, and between them the scales of a step 0
+    // in flight behind the next stage: two later ones, and between them the scales of a step 0
     stage_ready<2 * kLoads + (s == 1 || s == 2 ? kScaleLoads : 0)>();
-    if constexpr (s == 0) load_scales(kt / 4 + 1);
+    if constexpr (s == 0) load_scales(parity ^ 1, ahead / 4);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
+      for (int j = 0; j < FM; ++j) {
         mma<s, FM == 8>(acc[i][j], fb[cur][j], fa[cur][i], sb[j], sa[i]);
         __builtin_amdgcn_sched_barrier(0);
-        if (j == FN / 4 - (FN == 2 ? 0 : 1)) fa[nxt][i] = stage[(s + 1) % kStages][wm * FM + i][lane];
-        if (j == FN / 2 - 1) fb[nxt][i] = stage[(s + 1) % kStages][2 * FM + wn * FN + i][lane];
-        if (j == 3 * FN / 4 - 1 && i < kLoads) load_part(kt + 4, i);
-        if (s == 3 && j == FN - 1) {
-          sna[i] = scales[(kt / 4 + 1) % 2][wm * FM + i][lane];
-          snb[i] = scales[(kt / 4 + 1) % 2][2 * FM + wn * FN + i][lane];
+        if (j == FM / 4 - (FM == 2 ? 0 : 1)) fa[nxt][i] = stage[(s + 1) % kStages][wm * FM + i][lane];
+        if (j == FM / 2 - 1) fb[nxt][i] = stage[(s + 1) % kStages][kSide + wn * FM + i][lane];
+        if (j == 3 * FM / 4 - 1 && i < kLoads) load_part(s, ahead + s, i);
+        if (s == 3 && j == FM - 1) {
+          sna[i] = scales[parity ^ 1][wm * FM + i][lane];
+          snb[i] = scales[parity ^ 1][kSide + wn * FM + i][lane];
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -212,59 +238,79 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
       for (int i = 0; i < FM; ++i) sa[i] = sna[i], sb[i] = snb[i];
     }
   };
-  for (int kt = 0; kt < KT; kt += kStages) {
-    step(std::integral_constant<int, 0>{}, kt);
-    step(std::integral_constant<int, 1>{}, kt + 1);
-    step(std::integral_constant<int, 2>{}, kt + 2);
-    step(std::integral_constant<int, 3>{}, kt + 3);
-    if (FM == 8 && kt + kStages >= KT) mma_done();
-  }
-  stage_ready<0>();  // no load to LDS is on its way, and no wave reads a stage any more
-
-  // A wave's part of C, when it lies inside: through LDS, rows of whole lines out of it.  Else element by element.
-  const int64_t row0 = (rt_a + wm * FM) * kTileRows, col0 = (rt_b + wn * FN) * kTileRows;
-  if (row0 + FM * 16 <= a.rows && col0 + FN * 16 <= b.rows) {
-    constexpr int kBytes = Elem<TYPE>::kBytes, kPitch = FN * 16 * kBytes + 16;
-    constexpr int kRound = TYPE == EMB_TYPE_FP32 && FM > 2 ? FM / 4 : FM / 2;   // row tiles at a time
-    constexpr int kLanes = FN * 16 * kBytes / 16, kRows = 64 / kLanes;  // lanes a row, rows an access
-    static_assert(4 * kRound * 16 * kPitch <= (int)sizeof(stage));
-    uint8_t* own = reinterpret_cast<uint8_t*>(&stage[0][0][0]) + wave * (kRound * 16 * kPitch);
-    typename Elem<TYPE>::type* out = c + (row0 + lane / kLanes) * ldc + col0 + lane % kLanes * (16 / kBytes);
-#pragma unroll
-    for (int r = 0; r < FM; r += kRound) {
-#pragma unroll
-      for (int i = 0; i < kRound; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          uint8_t* p = own + (i * 16 + (lane & 15)) * kPitch + (j * 16 + (lane >> 4) * 4) * kBytes;
-          const f32x4 v = acc[r + i][j];
-          if constexpr (TYPE == EMB_TYPE_FP32)
-            *reinterpret_cast<f32x4*>(p) = v;
-          else
-            *reinterpret_cast<uint2*>(p) = make_uint2(to_bits<TYPE>(v[0]) | to_bits<TYPE>(v[1]) << 16,
-                                                      to_bits<TYPE>(v[2]) | to_bits<TYPE>(v[3]) << 16);
-        }
-      asm volatile("" : : : "memory");
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int i = 0; i < kRound * 16; i += kRows) {
-        const v4i v = *reinterpret_cast<const v4i*>(own + (i + lane / kLanes) * kPitch + lane % kLanes * 16);
-        const Bytes16 w = {{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]}};
-        *reinterpret_cast<Bytes16*>(out + (r * 16 + i) * ldc) = w;
+  for (;;) {
+    const int64_t row0 = (rt_a + wm * FM) * kTileRows, col0 = (rt_b + wn * FM) * kTileRows;
+    nth += stride;
+    const bool more = kStays<FM> && nth < run;
+    for (int kt = 0; kt < KT; kt += kStages) {
+      int ahead = kt + kStages;
+      if (more && ahead >= KT) {  // the last group loads the first of the next tile
+        place(nth, &rt_a, &rt_b);
+        aim(rt_a, rt_b);
+        ahead = 0;
       }
-      asm volatile("" : : : "memory");
-      __builtin_amdgcn_wave_barrier();
+      step(std::integral_constant<int, 0>{}, ahead);
+      step(std::integral_constant<int, 1>{}, ahead);
+      step(std::integral_constant<int, 2>{}, ahead);
+      step(std::integral_constant<int, 3>{}, ahead);
+      parity ^= 1;
+      if (FM == 8 && kt + kStages >= KT) mma_done();
     }
-    return;
+    if (!kStays<FM>) stage_ready<0>();  // the stages are free
+
+    // A wave's part of C, where it lies inside: whole lines out of LDS (16-byte pieces of a row exchanged by the row's
+    // number, so that no bank is hit twice).  Elsewhere element by element.
+    int l = lane;
+    asm volatile("" : "+v"(l));  // or the addresses below would be computed ahead of all tiles, and kept
+    if (row0 + FM * 16 <= a.rows && col0 + FM * 16 <= b.rows) {
+      uint8_t* own = kStays<FM> ? reinterpret_cast<uint8_t*>(&leave[kStays<FM> ? wave : 0][0])
+                                : reinterpret_cast<uint8_t*>(&stage[0][0][0]) + wave * 4096;
+      typename Elem<TYPE>::type* out = c + (row0 + l / kLanes) * ldc + col0 + l % kLanes * (16 / kBytes);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j0 = 0; j0 < FM; j0 += kOutCols / 16) {
+#pragma unroll
+          for (int j = 0; j < kOutCols / 16; ++j) {
+            const int at = (j * 16 + (l >> 4) * 4) * kBytes;
+            uint8_t* p = own + (l & 15) * (kOutCols * kBytes) + ((at / 16 ^ l) % kLanes) * 16 + at % 16;
+            const f32x4 v = fetched<FM>(acc[i][j0 + j]);
+            if constexpr (TYPE == EMB_TYPE_FP32)
+              *reinterpret_cast<f32x4*>(p) = v;
+            else
+              *reinterpret_cast<uint2*>(p) = make_uint2(to_bits<TYPE>(v[0]) | to_bits<TYPE>(v[1]) << 16,
+                                                        to_bits<TYPE>(v[2]) | to_bits<TYPE>(v[3]) << 16);
+          }
+          asm volatile("" : : : "memory");
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int r0 = 0; r0 < 16; r0 += kRows) {
+            const int r = r0 + l / kLanes;
+            const v4i v = *reinterpret_cast<const v4i*>(own + r * (kOutCols * kBytes) + ((l ^ r) % kLanes) * 16);
+            const Bytes16 w = {{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]}};
+            *reinterpret_cast<Bytes16*>(out + (i * 16 + r0) * ldc + j0 * 16) = w;
+          }
+          asm volatile("" : : : "memory");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_sched_barrier(0);  // accumulators are fetched as they leave
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+          const int64_t row = row0 + i * kTileRows + (l & 15);
+          const int64_t col = col0 + j * kTileRows + (l >> 4) * 4;
+          if (row < a.rows && col < b.rows) store4<TYPE>(c + row * ldc, col, b.rows, fetched<FM>(acc[i][j]));
+        }
+    }
+    if (!more) break;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int64_t row = row0 + i * kTileRows + (lane & 15);
-      const int64_t col = col0 + j * kTileRows + (lane >> 4) * 4;
-      if (row < a.rows && col < b.rows) store4<TYPE>(c + row * ldc, col, b.rows, acc[i][j]);
-    }
+  if (kStays<FM>) stage_ready<0>();  // no load to LDS outlives the workgroup
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -446,13 +492,14 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
     return qb.row_tiles < qa.row_tiles ? skinny<-1, TYPE, true>(qa, qb, FullRows{}, c, ldc, s)
                                        : skinny<-1, TYPE, false>(qb, qa, FullRows{}, c, ldc, s);
   const int f = tile_side(qa, qb);
-  const unsigned grid = (unsigned)tiles_of(qa, qb, f);
+  const int64_t tiles = tiles_of(qa, qb, f);
+  const unsigned grid = (unsigned)(f == 8 && tiles > kResident ? kResident : tiles);
   if (f == 8)
-    k_product<TYPE, 8, 8><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 8><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   else if (f == 4)
-    k_product<TYPE, 4, 4><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 4><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   else
-    k_product<TYPE, 2, 2><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
+    k_product<TYPE, 2><<<grid, 256, 0, s>>>(qa, qb, c, ldc);
   return hipGetLastError();
 }
 

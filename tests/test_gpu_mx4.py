@@ -183,6 +183,25 @@ def test_matmul(torch, m, n, k):
         assert torch.equal(mx4.matmul(a4, b4, dtype=getattr(torch, dtype)), got)   # same bits again
 
 
+@pytest.mark.parametrize("m,n,k", [(8100, 4090, 130), (8192, 4096, 512), (8100, 4090, 1100), (4090, 8192, 600)])
+def test_matmul_of_more_tiles_than_workgroups(torch, m, n, k):
+    """Tiles of 256 x 256 that a workgroup takes one after the other, whole and ragged, with an odd and an even number
+    of column groups; the 64-bit product on the GPU."""
+    from paper_2010_11305_amd import mx4
+
+    print("many tiles", m, n, k, flush=True)
+    a4, b4 = mx4.quantize(matrix(torch, m, k, "float32", m + k)), mx4.quantize(matrix(torch, n, k, "float32", n * k + 1))
+    a, b = a4.dequantize().double(), b4.dequantize().double()
+    want, sums = a @ b.t(), a.abs() @ b.abs().t()
+    for dtype in ("float32", "bfloat16"):
+        bound = k * 2.0**-23 * sums + ROUND[dtype] * want.abs()
+        out = torch.full((m, n + 3), 9.0, dtype=getattr(torch, dtype), device="cuda")
+        got = mx4.matmul(a4, b4, out=out[:, 1:n + 1])
+        assert bool(((got.double() - want).abs() <= bound).all())
+        assert bool((out[:, 0] == 9.0).all()) and bool((out[:, n + 1:] == 9.0).all())
+        assert torch.equal(mx4.matmul(a4, b4, dtype=getattr(torch, dtype)), got)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 40, 200), (20, 300, 700), (300, 270, 600)])
 def test_not_finite_blocks_reach_their_rows_alone(torch, m, n, k):
     """A NaN or infinity makes its block NaN, and with it exactly the outputs of its row (or column)."""
