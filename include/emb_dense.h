@@ -182,7 +182,8 @@ int emb_adamw_destroy(emb_adamw_t h);
  * the call only), each tensor contiguous, at any alignment of its type.  A tensor whose
  * gradient is NULL keeps its parameters and moments.  grad_scale: a device FP32 factor of
  * every gradient (what a clipped norm leaves, say), or NULL for 1.  The step counter
- * increases by one.  Enqueue-only. */
+ * increases by one; it lives on the host, so a call captured into a HIP graph repeats the
+ * constants and draws of the step it was captured in.  Enqueue-only. */
 int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads, double lr, const float* grad_scale,
                    void* stream);
 

@@ -3,16 +3,20 @@
     opt = adamw.AdamW(params, lr=1e-3, state_bits=8, rounding="stochastic")
     opt.step(grads)            # or opt.step(grads, lr=..., grad_scale=clip_factor)
 
-Parameters are updated in place.  The update runs in one HIP kernel per 192 tensors.
+Parameters are updated in place.  The update runs in one HIP kernel per 240 tensors.
 """
 from __future__ import annotations
 
 import ctypes
 from array import array
+from operator import attrgetter
 
 import torch
+from torch import Tensor
 
 from . import dense_lib as lib
+
+dtype_of = attrgetter("dtype")
 
 
 class AdamW:
@@ -74,17 +78,22 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
-        gd, index = self.grad_dtype, self.device.index
-        for g, n in zip(grads, self.sizes):
-            if g is not None and (g.dtype != gd or g.numel() != n or g.get_device() != index or not g.is_contiguous()):
-                raise ValueError(f"a gradient must be contiguous, {gd}, on {self.device}, and as large as its parameter")
+        # a model has hundreds of tensors and a step lasts some hundred microseconds: C-level maps, one a property
+        given, sizes = grads, self.sizes
+        if any(g is None for g in grads):
+            kept = [k for k, g in enumerate(grads) if g is not None]
+            given, sizes = [grads[k] for k in kept], [sizes[k] for k in kept]
+        index = self.device.index
+        if (list(map(Tensor.numel, given)) != sizes or not all(map(Tensor.is_contiguous, given))
+                or not set(map(dtype_of, given)) <= {self.grad_dtype} or not set(map(Tensor.get_device, given)) <= {index}):
+            raise ValueError(f"gradients must be contiguous, {self.grad_dtype}, on {self.device}, and each as large as its parameter")
         scale = None
         if grad_scale is not None:
             if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != index:
                 raise ValueError(f"grad_scale must be one float32 value on {self.device}")
             scale = grad_scale.data_ptr()
-        pp = array("Q", [p.data_ptr() for p in self.params])
-        gp = array("Q", [0 if g is None else g.data_ptr() for g in grads])
+        pp = array("Q", map(Tensor.data_ptr, self.params))
+        gp = array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
         lib.call("emb_adamw_step", self.device, self._h, pp.buffer_info()[0], gp.buffer_info()[0],
                  self.lr if lr is None else float(lr), scale)
 

@@ -25,7 +25,8 @@ bool rounding_ok(int32_t r) { return r == EMB_ROUND_NEAREST || r == EMB_ROUND_ST
 // Sizes an MX4 matrix may have: below 2^31 each way, and a buffer that can exist.
 bool dims_ok(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0 || rows >= kMaxDim || cols >= kMaxDim) return false;
-  return (double)(rows + kTileRows) * (double)(cols + kTileCols * kScaleTiles) <= kMaxBytes;
+  const Mx4 q(nullptr, rows, cols);   // at most 2^27 row tiles of 2^24 column tiles: no overflow of 64 bits
+  return (double)q.bytes() <= kMaxBytes;
 }
 
 // The operands of a product.

@@ -60,7 +60,7 @@ hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t 
 
 // ---- AdamW -----------------------------------------------------------------------------------
 constexpr int kAdamChunk = 4096;     // elements of a tensor that one workgroup updates
-constexpr int kAdamTensors = 192;    // tensors whose pointers one launch carries (kernel arguments hold 4 KB)
+constexpr int kAdamTensors = 240;    // tensors whose pointers one launch carries (kernel arguments hold 4 KB)
 
 struct AdamTensor {
   int64_t base;    // first element in the state

@@ -33,7 +33,7 @@ def test_every_declared_symbol_is_exported(L):
         assert ctypes.cast(getattr(L, n), ctypes.c_void_p).value
 
 
-@pytest.mark.parametrize("rows,cols", [(1, 1), (16, 128), (17, 129), (4096, 12800), (1000, 1999), (5, 513)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (16, 128), (17, 129), (4096, 12800), (1000, 1999), (5, 513), (2**31 - 1, 1), (1, 2**31 - 1)])
 def test_mx4_bytes(L, rows, cols):
     n = ctypes.c_size_t()
     assert L.emb_mx4_query_bytes(rows, cols, ctypes.byref(n)) == 0

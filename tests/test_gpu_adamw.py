@@ -206,7 +206,7 @@ def test_many_tensors(torch, bits):
     opt = AdamW(params, lr=LR, state_bits=bits)
     for _ in range(2):
         opt.step(grads)
-    for k in (0, 100, 191, 192, 193, 383, 384, 449, 450):
+    for k in (0, 100, 191, 192, 193, 239, 240, 241, 383, 384, 449, 450):
         one = AdamW([alone[k]], lr=LR, state_bits=bits)
         for _ in range(2):
             one.step([grads[k]])
