@@ -59,7 +59,9 @@ hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t 
                          int64_t ldy, void* workspace, hipStream_t s);
 
 // ---- AdamW -----------------------------------------------------------------------------------
-constexpr int kAdamChunk = 4096;     // elements of a tensor that one workgroup updates
+constexpr int kAdamThreads = 256;
+constexpr int kAdamPer = 8;          // elements of a thread
+constexpr int kAdamChunk = kAdamThreads * kAdamPer;   // elements of a tensor that one workgroup updates
 constexpr int kAdamTensors = 240;    // tensors whose pointers one launch carries (kernel arguments hold 4 KB)
 
 struct AdamTensor {

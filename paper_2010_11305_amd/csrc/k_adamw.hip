@@ -12,7 +12,7 @@ namespace embd {
 
 namespace {
 
-constexpr int kPer = 8;
+constexpr int kPer = kAdamPer;
 using s16x2 = short __attribute__((ext_vector_type(2)));
 
 // The largest of a value over the 4 lanes of a quad.
@@ -88,7 +88,7 @@ __device__ __forceinline__ void e4m3_unpack(uint2 w, uint32_t scale, float (&x)[
 }
 
 template <int PT, int GT, int BITS, bool STOCHASTIC>
-__global__ __launch_bounds__(256) void k_adamw(AdamDev d, AdamPointers ptr, uint32_t first, int64_t part0, AdamConst c,
+__global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamDev d, AdamPointers ptr, uint32_t first, int64_t part0, AdamConst c,
                                                const float* __restrict__ grad_scale) {
   const AdamPart part = d.parts[part0 + blockIdx.x];
   const uint32_t slot = part.tensor - first;
@@ -100,103 +100,100 @@ __global__ __launch_bounds__(256) void k_adamw(AdamDev d, AdamPointers ptr, uint
   const AdamTensor t = d.tensors[part.tensor];
   const float keep = (float)(1.0 - c.lr * t.decay);
   const float gs = grad_scale ? *grad_scale : 1.0f;
+  const int64_t i = (int64_t)part.chunk * kAdamChunk + threadIdx.x * kPer;
+  // a block of 32 that the tensor reaches into is worked on by its whole quad
+  if (i >= (t.size + kBlock - 1) / kBlock * kBlock) return;
+  const int n = t.size - i >= kPer ? kPer : t.size > i ? (int)(t.size - i) : 0;
+  Raw<PT, kPer> rp;
+  Raw<GT, kPer> rg;
+  load_values(p + (n ? i : 0), n, rp);
+  load_values(g + (n ? i : 0), n, rg);
+  const int64_t at = t.base + i;
+  float m[kPer], v[kPer];
+  if constexpr (BITS == 32) {
+    const float4* sm = reinterpret_cast<const float4*>(d.first) + at / 4;
+    const float4* sv = reinterpret_cast<const float4*>(d.second) + at / 4;
 #pragma unroll
-  for (int it = 0; it < kAdamChunk / (256 * kPer); ++it) {
-    const int64_t i = (int64_t)part.chunk * kAdamChunk + (it * 256 + threadIdx.x) * kPer;
-    // a block of 32 that the tensor reaches into is worked on by its whole quad
-    if (i >= (t.size + kBlock - 1) / kBlock * kBlock) return;
-    const int n = t.size - i >= kPer ? kPer : t.size > i ? (int)(t.size - i) : 0;
-    Raw<PT, kPer> rp;
-    Raw<GT, kPer> rg;
-    load_values(p + (n ? i : 0), n, rp);
-    load_values(g + (n ? i : 0), n, rg);
-    const int64_t at = t.base + i;
-    float m[kPer], v[kPer];
-    if constexpr (BITS == 32) {
-      const float4* sm = reinterpret_cast<const float4*>(d.first) + at / 4;
-      const float4* sv = reinterpret_cast<const float4*>(d.second) + at / 4;
+    for (int h = 0; h < 2; ++h) {
+      const float4 a = sm[h], b = sv[h];
+      m[4 * h] = a.x, m[4 * h + 1] = a.y, m[4 * h + 2] = a.z, m[4 * h + 3] = a.w;
+      v[4 * h] = b.x, v[4 * h + 1] = b.y, v[4 * h + 2] = b.z, v[4 * h + 3] = b.w;
+    }
+  } else {
+    const uint2 a = *reinterpret_cast<const uint2*>(d.first + at), b = *reinterpret_cast<const uint2*>(d.second + at);
+    e4m3_unpack(a, d.first_scale[at / kBlock], m);
+    e4m3_unpack(b, d.second_scale[at / kBlock], v);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float4 a = sm[h], b = sv[h];
-        m[4 * h] = a.x, m[4 * h + 1] = a.y, m[4 * h + 2] = a.z, m[4 * h + 3] = a.w;
-        v[4 * h] = b.x, v[4 * h + 1] = b.y, v[4 * h + 2] = b.z, v[4 * h + 3] = b.w;
-      }
+    for (int j = 0; j < kPer; ++j) v[j] = v[j] * v[j];
+  }
+  uint32_t word[kPer] = {};
+  if constexpr (STOCHASTIC) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t n4 = (uint64_t)(at / 4 + h);
+      const uint4 w = philox(make_uint4((uint32_t)n4, (uint32_t)(n4 >> 32), c.t, 0), c.k0, c.k1);
+      word[4 * h] = w.x, word[4 * h + 1] = w.y, word[4 * h + 2] = w.z, word[4 * h + 3] = w.w;
+    }
+  }
+  float root[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const float gj = rg.get(j) * gs;
+    m[j] = m[j] * c.beta1 + gj * c.rest1;
+    v[j] = v[j] * c.beta2 + (gj * gj) * c.rest2;
+    root[j] = sqrtf(v[j]);
+    const float away = m[j] / (root[j] * c.inv_root + c.eps);
+    const float x = rp.get(j) * keep - away * c.rate;
+    if constexpr (PT == EMB_TYPE_FP32) {
+      rp.w[j] = __float_as_uint(x);
+    } else if constexpr (STOCHASTIC) {
+      const uint32_t b = __float_as_uint(x), u = (word[j] ^ word[j] >> 16) & 0xFFFFu;
+      const bool whole = (b & 0x7F800000u) == 0x7F800000u;  // infinities and NaN are kept
+      rp.put(j, whole ? bf16_bits(x) : (b + u) >> 16);
     } else {
-      const uint2 a = *reinterpret_cast<const uint2*>(d.first + at), b = *reinterpret_cast<const uint2*>(d.second + at);
-      e4m3_unpack(a, d.first_scale[at / kBlock], m);
-      e4m3_unpack(b, d.second_scale[at / kBlock], v);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) v[j] = v[j] * v[j];
+      rp.put(j, bf16_bits(x));
     }
-    uint32_t word[kPer] = {};
-    if constexpr (STOCHASTIC) {
+  }
+  if (n < kPer) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint64_t n4 = (uint64_t)(at / 4 + h);
-        const uint4 w = philox(make_uint4((uint32_t)n4, (uint32_t)(n4 >> 32), c.t, 0), c.k0, c.k1);
-        word[4 * h] = w.x, word[4 * h + 1] = w.y, word[4 * h + 2] = w.z, word[4 * h + 3] = w.w;
-      }
+    for (int j = 0; j < kPer; ++j)
+      if (j >= n) m[j] = 0.0f, v[j] = 0.0f, root[j] = 0.0f;
+  }
+  if (n == kPer) {
+#pragma unroll
+    for (int h = 0; h < Raw<PT, kPer>::kWords / 4; ++h) {
+      const Bytes16 b = {{rp.w[4 * h], rp.w[4 * h + 1], rp.w[4 * h + 2], rp.w[4 * h + 3]}};
+      reinterpret_cast<Bytes16*>(p + i)[h] = b;
     }
-    float root[kPer];
+  } else {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const float gj = rg.get(j) * gs;
-      m[j] = m[j] * c.beta1 + gj * c.rest1;
-      v[j] = v[j] * c.beta2 + (gj * gj) * c.rest2;
-      root[j] = sqrtf(v[j]);
-      const float away = m[j] / (root[j] * c.inv_root + c.eps);
-      const float x = rp.get(j) * keep - away * c.rate;
-      if constexpr (PT == EMB_TYPE_FP32) {
-        rp.w[j] = __float_as_uint(x);
-      } else if constexpr (STOCHASTIC) {
-        const uint32_t b = __float_as_uint(x), u = (word[j] ^ word[j] >> 16) & 0xFFFFu;
-        const bool whole = (b & 0x7F800000u) == 0x7F800000u;  // infinities and NaN are kept
-        rp.put(j, whole ? bf16_bits(x) : (b + u) >> 16);
-      } else {
-        rp.put(j, bf16_bits(x));
-      }
+      if (j >= n) continue;
+      if constexpr (PT == EMB_TYPE_FP32)
+        p[i + j] = __uint_as_float(rp.w[j]);
+      else
+        p[i + j] = (uint16_t)(j % 2 ? rp.w[j / 2] >> 16 : rp.w[j / 2]);
     }
-    if (n < kPer) {
+  }
+  if constexpr (BITS == 32) {
+    float4* sm = reinterpret_cast<float4*>(d.first) + at / 4;
+    float4* sv = reinterpret_cast<float4*>(d.second) + at / 4;
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (j >= n) m[j] = 0.0f, v[j] = 0.0f, root[j] = 0.0f;
+    for (int h = 0; h < 2; ++h) {
+      sm[h] = make_float4(m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]);
+      sv[h] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
     }
-    if (n == kPer) {
+  } else {
+    uint32_t um[kPer], ur[kPer], s1, s2;
 #pragma unroll
-      for (int h = 0; h < Raw<PT, kPer>::kWords / 4; ++h) {
-        const Bytes16 b = {{rp.w[4 * h], rp.w[4 * h + 1], rp.w[4 * h + 2], rp.w[4 * h + 3]}};
-        reinterpret_cast<Bytes16*>(p + i)[h] = b;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        if (j >= n) continue;
-        if constexpr (PT == EMB_TYPE_FP32)
-          p[i + j] = __uint_as_float(rp.w[j]);
-        else
-          p[i + j] = (uint16_t)(j % 2 ? rp.w[j / 2] >> 16 : rp.w[j / 2]);
-      }
-    }
-    if constexpr (BITS == 32) {
-      float4* sm = reinterpret_cast<float4*>(d.first) + at / 4;
-      float4* sv = reinterpret_cast<float4*>(d.second) + at / 4;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        sm[h] = make_float4(m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]);
-        sv[h] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
-      }
-    } else {
-      uint32_t um[kPer], ur[kPer], s1, s2;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) um[j] = ~word[j] << 16, ur[j] = ~word[j];
-      const uint2 a = e4m3_pack<STOCHASTIC, false>(m, um, &s1);
-      const uint2 b = e4m3_pack<STOCHASTIC, true>(root, ur, &s2);
-      *reinterpret_cast<uint2*>(d.first + at) = a;
-      *reinterpret_cast<uint2*>(d.second + at) = b;
-      if (threadIdx.x % 4 == 0) {
-        d.first_scale[at / kBlock] = (uint8_t)s1;
-        d.second_scale[at / kBlock] = (uint8_t)s2;
-      }
+    for (int j = 0; j < kPer; ++j) um[j] = ~word[j] << 16, ur[j] = ~word[j];
+    const uint2 a = e4m3_pack<STOCHASTIC, false>(m, um, &s1);
+    const uint2 b = e4m3_pack<STOCHASTIC, true>(root, ur, &s2);
+    *reinterpret_cast<uint2*>(d.first + at) = a;
+    *reinterpret_cast<uint2*>(d.second + at) = b;
+    if (threadIdx.x % 4 == 0) {
+      d.first_scale[at / kBlock] = (uint8_t)s1;
+      d.second_scale[at / kBlock] = (uint8_t)s2;
     }
   }
 }
@@ -209,15 +206,15 @@ hipError_t adamw_as(const AdamDev& d, const AdamPointers& ptr, uint32_t first, i
   if (bits == 32) {
     if constexpr (PT != EMB_TYPE_FP32) {
       if (random) {
-        k_adamw<PT, GT, 32, true><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+        k_adamw<PT, GT, 32, true><<<grid, kAdamThreads, 0, s>>>(d, ptr, first, part0, c, gs);
         return hipGetLastError();
       }
     }
-    k_adamw<PT, GT, 32, false><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+    k_adamw<PT, GT, 32, false><<<grid, kAdamThreads, 0, s>>>(d, ptr, first, part0, c, gs);
   } else if (random) {
-    k_adamw<PT, GT, 8, true><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+    k_adamw<PT, GT, 8, true><<<grid, kAdamThreads, 0, s>>>(d, ptr, first, part0, c, gs);
   } else {
-    k_adamw<PT, GT, 8, false><<<grid, 256, 0, s>>>(d, ptr, first, part0, c, gs);
+    k_adamw<PT, GT, 8, false><<<grid, kAdamThreads, 0, s>>>(d, ptr, first, part0, c, gs);
   }
   return hipGetLastError();
 }
