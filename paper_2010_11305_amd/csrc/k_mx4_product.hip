@@ -1,4 +1,13 @@
-// Products of MX4 matrices on the scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4.
+// Products of MX4 matrices on the scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4: a lane's
+// operand is one block, 32 codes in four registers, and its scale one byte of a register, which the layout of
+// an MX4 matrix holds lane by lane.  Codes and scales go from memory to the instruction as they lie.
+//
+// k_product: tiles of C of 256, 128 or 64 rows and columns, the operands staged in LDS.  16384 x 8192 x 12800: 642 to
+// 740 us from card to card, 5.4 to 4.6 PFLOP/s.  The bound is power: on normal values the clock falls from 2.4 to
+// 1.6 GHz (560 us and 2.4 GHz on zeros, where a step takes 1190 cycles of the 1024 that its instructions issue for).
+// The 32x32x64 instruction needs 6% fewer cycles and takes 2% longer.
+// k_skinny: few rows against a weight that is read once.  1 row, 4096 x 12800: 5.3 us for 27.9 MB, much of it
+// from the last-level cache; 1 row, 32000 x 4096: 14.9 us, 4.7 TB/s.
 #include <type_traits>
 
 #include "dense_device.h"
