@@ -47,15 +47,15 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
   using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
   constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = kTileCols / kPiece;
   __shared__ __attribute__((aligned(16))) E stage[St::kRows * kPitch];
-  const int64_t wide = (qr.cols + kTileCols * St::kSquareCols - 1) / (kTileCols * St::kSquareCols);
-  int64_t square = blockIdx.x / St::kSquare;
-  int in = blockIdx.x % St::kSquare;
+  const uint32_t wide = (uint32_t)((qr.cols + kTileCols * St::kSquareCols - 1) / (kTileCols * St::kSquareCols));
+  uint32_t square = blockIdx.x / St::kSquare, in = blockIdx.x % St::kSquare;
   if (gridDim.x >= St::kSquaresFrom * St::kSquare) {  // workgroups go to the XCDs in turn
-    square = (int64_t)blockIdx.x / (8 * St::kSquare) * 8 + blockIdx.x % 8;
+    square = blockIdx.x / (8 * St::kSquare) * 8 + blockIdx.x % 8;
     in = blockIdx.x / 8 % St::kSquare;
   }
-  const int64_t row0 = (square / wide * St::kSquareRows + in / St::kSquareCols) * St::kRows;
-  const int64_t kt0 = square % wide * St::kSquareCols + in % St::kSquareCols, col0 = kt0 * kTileCols;
+  // counts of workgroups and tiles are below 2^31: divisions of 32 bits
+  const int64_t row0 = ((int64_t)(square / wide) * St::kSquareRows + in / St::kSquareCols) * St::kRows;
+  const int64_t kt0 = (int64_t)(square % wide) * St::kSquareCols + in % St::kSquareCols, col0 = kt0 * kTileCols;
   // by columns the rows go on to the end of their tile of 128
   const int64_t row_end = BY_COLUMNS ? qc.col_tiles * kTileCols : qr.row_tiles * kTileRows;
   if (row0 >= row_end || kt0 >= qr.col_tiles) return;
@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
 // tile, so that a wave writes whole lines.
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::type* __restrict__ x, int64_t ld) {
-  const int64_t tile = blockIdx.x;
-  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const uint32_t wide = (uint32_t)q.col_tiles;
+  const int64_t rt = blockIdx.x / wide, kt = blockIdx.x % wide;
   const int rr = threadIdx.x >> 4, c8 = threadIdx.x & 15, lane = (c8 >> 2) * 16 + rr;
   const int64_t row = rt * kTileRows + rr, col = kt * kTileCols + c8 * 8;
   if (row >= q.rows || col >= q.cols) return;
@@ -143,10 +143,10 @@ __global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::
 // Plain codes to tiles and back: a thread takes one block.
 __global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                               Mx4 q, uint8_t* __restrict__ out) {
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
   if (tile >= q.row_tiles * q.col_tiles) return;
   const int lane = threadIdx.x & 63;
-  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int64_t rt = tile / wide, kt = tile % wide;
   const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
   const int64_t left = row < q.rows ? q.cols - col : 0;
   const int n = (int)(left < 0 ? 0 : left > kBlock ? kBlock : left);
@@ -168,10 +168,10 @@ __global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes,
 }
 
 __global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
   if (tile >= q.row_tiles * q.col_tiles) return;
   const int lane = threadIdx.x & 63;
-  const int64_t rt = tile / q.col_tiles, kt = tile % q.col_tiles;
+  const int64_t rt = tile / wide, kt = tile % wide;
   const int64_t row = rt * kTileRows + (lane & 15), col = kt * kTileCols + (lane >> 4) * kBlock;
   const int64_t left = row < q.rows ? q.cols - col : 0;
   if (left <= 0) return;

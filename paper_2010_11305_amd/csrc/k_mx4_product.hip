@@ -151,16 +151,17 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
 
   // Workgroups go to the XCDs in turn.  Each XCD takes a run of consecutive tiles, in bands of 8 tile rows, so that what
   // its L2 holds is used by the workgroups that run there together.
-  const int64_t mt_all = (a.row_tiles + kSide - 1) / kSide, nt_all = (b.row_tiles + kSide - 1) / kSide;
-  const int64_t total = mt_all * nt_all, xcd = blockIdx.x % 8;
-  const int64_t run0 = xcd * (total / 8) + (xcd < total % 8 ? xcd : total % 8);
-  const int64_t run = total / 8 + (xcd < total % 8 ? 1 : 0);
-  const int64_t stride = (gridDim.x + 7) / 8;
-  const auto place = [&](int64_t nth, int64_t* rt_a, int64_t* rt_b) {
-    const int64_t id = run0 + nth, band = id / (8 * nt_all), in_band = id % (8 * nt_all);
-    const int64_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
-    *rt_a = (band * 8 + in_band % band_rows) * kSide;
-    *rt_b = in_band / band_rows * kSide;
+  // Their number is below 2^31.
+  const uint32_t mt_all = (uint32_t)((a.row_tiles + kSide - 1) / kSide), nt_all = (uint32_t)((b.row_tiles + kSide - 1) / kSide);
+  const uint32_t total = mt_all * nt_all, xcd = blockIdx.x % 8;
+  const uint32_t run0 = xcd * (total / 8) + (xcd < total % 8 ? xcd : total % 8);
+  const uint32_t run = total / 8 + (xcd < total % 8 ? 1 : 0);
+  const uint32_t stride = (gridDim.x + 7) / 8;
+  const auto place = [&](uint32_t nth, int64_t* rt_a, int64_t* rt_b) {
+    const uint32_t id = run0 + nth, band = id / (8 * nt_all), in_band = id % (8 * nt_all);
+    const uint32_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
+    *rt_a = (int64_t)(band * 8 + in_band % band_rows) * kSide;
+    *rt_b = (int64_t)(in_band / band_rows) * kSide;
   };
 
   const int KT = (int)a.col_tiles, KG = (int)a.col_groups;
@@ -198,7 +199,8 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
       load_to_lds(scales_at + parity * (kTiles * 256) + i * 1024, scale_at[i], scale_srd, k * kScaleBytes);
   };
 
-  int64_t nth = blockIdx.x / 8, rt_a, rt_b;
+  uint32_t nth = blockIdx.x / 8;
+  int64_t rt_a, rt_b;
   place(nth, &rt_a, &rt_b);
   aim(rt_a, rt_b);
   f32x4 acc[FM][FM] = {};
