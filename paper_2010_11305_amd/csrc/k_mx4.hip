@@ -1,10 +1,10 @@
 // MX4 matrices: quantisation by rows and by columns, expansion, and the plain codes.
 //
-// Rounding to nearest and expansion are bound by memory.  16384 x 12800 BF16 (420 MB): by rows 102 us, by columns
-// 111 us, both 122 us (5.3 TB/s of the bytes that have to move; a copy of 1 GiB reaches 5.0); expansion to BF16
-// 116 us (4.6 TB/s).  FP32: 195, 200, 203 and 183 us.
-// Stochastic rounding is bound by the VALU: 137, 137 and 214 us.  Per value 5 of its 17 instructions are the
-// multiplications of Philox, which issue at a quarter of the rate: half of its time.
+// Rounding to nearest and expansion are bound by memory.  16384 x 12800 BF16 (420 MB): by rows 95 us, by columns
+// 100 us, both 122 to 127 us (5.1 to 5.6 TB/s of the bytes that have to move; a copy of 1 GiB reaches 5.0);
+// expansion to BF16 114 us (4.7 TB/s).  FP32: 174, 188, 203 and 181 us.
+// Stochastic rounding is bound by the VALU: 154, 151 and 214 to 218 us.  Per value 2.3 of its 17 instructions are the
+// multiplications of Philox, which issue at a quarter of the rate: two fifths of its time.
 #include "dense_device.h"
 
 namespace embd {
@@ -20,15 +20,16 @@ __device__ __forceinline__ void store_scale(uint8_t* out, const Mx4& q, int64_t 
     for (int t = (int)(kt % kScaleTiles) + 1; t < kScaleTiles; ++t) *++p = 0;
 }
 
-// A workgroup stages some rows x 128 columns of x in LDS, read in whole lines, and quantises them along the
+// A workgroup stages 32 rows x 128 columns of x in LDS, read in whole lines, and quantises them along the
 // rows, the columns or both: a thread takes 32 values that share a scale, so no step crosses lanes, and
 // writes its 16 bytes of codes where 16 threads make 256 contiguous ones.  For both, one half of
-// the threads takes the columns (a wave reads a row of the stage at a time) and the other the rows.
-template <int TYPE, bool BY_ROWS, bool BY_COLUMNS>
+// the threads takes the columns (a wave reads a row of the stage at a time) and the other the rows; for one
+// the other half only loads (256 x 416: 3.3 us, with 128 threads 3.9; 16384 x 12800: 95 us and 103).
+template <int TYPE, bool BY_COLUMNS>
 struct Stage {
   static constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
-  static constexpr int kRows = BY_COLUMNS ? kBlock : 64;
-  static constexpr int kThreads = BY_ROWS ? 256 : 128;
+  static constexpr int kRows = kBlock;
+  static constexpr int kThreads = 256;
   static constexpr int kPitch = kTileCols + kPiece;  // 16 more bytes a row: rows start in different banks
   // The scale bytes of four tiles along a quantised axis lie in one dword, and a column's codes of 128 rows in one
   // tile: where there are many workgroups those of 512 rows (by columns) x 512 columns run on one XCD, whose
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
                                                   int64_t ld, uint8_t* __restrict__ by_rows,
                                                   uint8_t* __restrict__ by_columns, Mx4Random rnd) {
   using E = typename Elem<TYPE>::type;
-  using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
+  using St = Stage<TYPE, BY_COLUMNS>;
   constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = kTileCols / kPiece;
   __shared__ __attribute__((aligned(16))) E stage[St::kRows * kPitch];
   const uint32_t wide = (uint32_t)((qr.cols + kTileCols * St::kSquareCols - 1) / (kTileCols * St::kSquareCols));
@@ -82,8 +83,8 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
     const int lane = (int)(row0 % kTileCols / kBlock) * 16 + (int)(col % kTileRows);
     *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
     store_scale(by_columns, qc, rt, kt, lane, s);
-  } else if constexpr (BY_ROWS) {
-    const int task = threadIdx.x - (BY_COLUMNS ? 128 : 0), rr = task % St::kRows, h = task / St::kRows;
+  } else if (BY_ROWS && (BY_COLUMNS || threadIdx.x < 128)) {
+    const int task = threadIdx.x % 128, rr = task % St::kRows, h = task / St::kRows;
     const int64_t row = row0 + rr, col = col0 + h * kBlock, rt = row / kTileRows;
     if (rt >= qr.row_tiles) return;
 #pragma unroll
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ cod
 template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
 hipError_t quantize_along(const void* x, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
                           const Mx4Random& rnd, hipStream_t s) {
-  using St = Stage<TYPE, BY_ROWS, BY_COLUMNS>;
+  using St = Stage<TYPE, BY_COLUMNS>;
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   const int64_t squares = up(rows, St::kRows * St::kSquareRows) * up(cols, kTileCols * St::kSquareCols);
   const int64_t grid = (squares >= St::kSquaresFrom ? up(squares, 8) * 8 : squares) * St::kSquare;
