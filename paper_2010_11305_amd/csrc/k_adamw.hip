@@ -47,8 +47,8 @@ template <bool STOCHASTIC, bool KEEP>
 __device__ __forceinline__ uint2 e4m3_pack(const float (&x)[kPer], const uint32_t (&rest)[kPer], uint32_t* scale) {
   uint32_t a = 0;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) a = max(a, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-  const uint32_t s = e4m3_scale(quad_max(a));
+  for (int j = 0; j < kPer; ++j) a = max(a, __float_as_uint(x[j]) & (KEEP ? ~0u : 0x7FFFFFFFu));  // a root has no sign,
+  const uint32_t s = e4m3_scale(quad_max(a) & 0x7FFFFFFFu);                                // unless it is NaN
   *scale = s;
   if (s == 255u) return make_uint2(0, 0);
   uint32_t w[2];
@@ -58,7 +58,8 @@ __device__ __forceinline__ uint2 e4m3_pack(const float (&x)[kPer], const uint32_
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       float z = ceilf(ldexpf(fabsf(x[j]), up));
-      z = KEEP ? (x[j] > 0.0f ? fmaxf(z, 0x1p20f) : 0.0f) : copysignf(z, x[j]);
+      // KEEP: 0 stays 0, what is above 0 (1 at least here) becomes 2^20 at least
+      z = KEEP ? __builtin_amdgcn_fmed3f(z, 0x1p20f, z * 0x1p20f) : copysignf(z, x[j]);
       c[j] = (uint32_t)__builtin_amdgcn_cvt_scalef32_sr_fp8_f32(0, z, rest[j] | 0xFFFFu, 0x1p29f, 0);
     }
 #pragma unroll
@@ -82,13 +83,17 @@ __device__ __forceinline__ uint2 e4m3_pack(const float (&x)[kPer], const uint32_
 }
 
 __device__ __forceinline__ void e4m3_unpack(uint2 w, uint32_t scale, float (&x)[kPer]) {
-  const float f = scale == 255u ? __uint_as_float(0x7FC00000u) : power_of(scale);
+  const float f = power_of(scale);
   const uint32_t ws[2] = {w.x, w.y};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)ws[i], false);
-    const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)ws[i], true);
-    x[4 * i] = lo[0] * f, x[4 * i + 1] = lo[1] * f, x[4 * i + 2] = hi[0] * f, x[4 * i + 3] = hi[1] * f;
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(ws[i], f, false);
+    const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(ws[i], f, true);
+    x[4 * i] = lo[0], x[4 * i + 1] = lo[1], x[4 * i + 2] = hi[0], x[4 * i + 3] = hi[1];
+  }
+  if (scale == 255u) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x[j] = __uint_as_float(0x7FC00000u);
   }
 }
 
@@ -153,8 +158,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamDev d, AdamPointers 
       rp.w[j] = __float_as_uint(x);
     } else if constexpr (STOCHASTIC) {
       const uint32_t b = __float_as_uint(x), u = (word[j] ^ word[j] >> 16) & 0xFFFFu;
-      const bool whole = (b & 0x7F800000u) == 0x7F800000u;  // infinities and NaN are kept
-      rp.put(j, whole ? bf16_bits(x) : (b + u) >> 16);
+      rp.put(j, x != x ? 0x7FC0u : (b + u) >> 16);  // an infinity has no low bits to carry from
     } else {
       rp.put(j, bf16_bits(x));
     }
