@@ -146,7 +146,7 @@ int emb_mx4_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k
 
 int emb_mx4_linear_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
   if (!bytes || !product_ok(m, n, k)) return EMB_EINVAL;
-  *bytes = m && n && k ? linear_workspace(m, k) : 0;
+  *bytes = m && n && k ? linear_workspace(m, n, k) : 0;
   return EMB_OK;
 }
 
@@ -156,7 +156,7 @@ int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ld
   if (m == 0 || n == 0) return EMB_OK;
   if (!matrix_ok(y, type, m, n, ldy)) return EMB_EINVAL;
   if (k && (!matrix_ok(x, type, m, k, ldx) || !w || !aligned(w))) return EMB_EINVAL;
-  const size_t need = k ? linear_workspace(m, k) : 0;
+  const size_t need = k ? linear_workspace(m, n, k) : 0;
   if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
   if (workspace_bytes < need) return EMB_ENOMEM;
   return status(launch_linear(x, type, m, k, ldx, w, n, y, ldy, workspace, S(stream)));

@@ -54,7 +54,7 @@ hipError_t launch_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* cod
 
 hipError_t launch_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* c, int type, int64_t ldc,
                          hipStream_t s);
-size_t linear_workspace(int64_t m, int64_t k);
+size_t linear_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                          int64_t ldy, void* workspace, hipStream_t s);
 

@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
 // the order of the waves.  XT >= 0: x is a full-precision matrix that every workgroup
 // quantises into LDS first, 32 values a thread, while the first group of w arrives.
 constexpr int kSkinnyWaves = 16;
-constexpr int kFusedValues = 32768;   // of x, most
+constexpr int kFusedValues = 65536;   // of x, most
 
 struct FullRows {
   const void* x;
@@ -514,8 +514,15 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
   return hipGetLastError();
 }
 
-// Rows that every workgroup of k_skinny quantises by itself.
-bool fused(int64_t m, int64_t k) { return m <= 64 && m * ((k + 511) / 512 * 512) <= kFusedValues; }
+// Rows that every workgroup of k_skinny quantises by itself: few values, and not too many workgroups that do.  It saves
+// a launch.  us among other calls, with the quantisation inside / as a launch of its own: 16 rows, 4096 x 4096
+// 7.3 / 12.1; 4 rows, 4096 x 12800 9.3 / 11.9; 64 rows, 1000 x 1000 8.3 / 12.1, 8192 x 512 10.7 / 12.1; past the line
+// 5 rows, 8192 x 12800 16.8 / 15.1; 64 rows, 16384 x 512 20.2 / 12.3; 16 rows, 16384 x 2048 13.3 / 12.1.
+// (Replayed from a graph a launch costs less: 7.7 / 6.4, 10.3 / 10.9, 8.9 / 8.0.)
+bool fused(int64_t m, int64_t n, int64_t k) {
+  const int64_t values = m * ((k + 511) / 512 * 512);
+  return m <= 64 && values <= kFusedValues && values * ((n + kTileRows - 1) / kTileRows) <= (int64_t)1 << 24;
+}
 
 }  // namespace
 
@@ -526,13 +533,13 @@ hipError_t launch_matmul(const void* a, const void* b, int64_t m, int64_t n, int
   return matmul_as<EMB_TYPE_FP16>(a, b, m, n, k, c, ldc, s);
 }
 
-size_t linear_workspace(int64_t m, int64_t k) {
-  return fused(m, k) ? 0 : (size_t)Mx4(nullptr, m, k).bytes();
+size_t linear_workspace(int64_t m, int64_t n, int64_t k) {
+  return fused(m, n, k) ? 0 : (size_t)Mx4(nullptr, m, k).bytes();
 }
 
 hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                          int64_t ldy, void* workspace, hipStream_t s) {
-  if (k && fused(m, k)) {
+  if (k && fused(m, n, k)) {
     const Mx4 qw(w, n, k), qx(nullptr, m, k);
     const FullRows full = {x, ldx};
     if (type == EMB_TYPE_FP32)

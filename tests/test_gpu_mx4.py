@@ -231,7 +231,9 @@ def test_extreme_scales(torch):
 
 
 LINEARS = [(1, 16, 16), (1, 33, 70), (1, 4096, 800), (2, 1000, 4100), (5, 64, 12800), (16, 128, 128), (17, 200, 999),
-           (33, 2000, 1000), (67, 300, 513), (200, 100, 2000), (512, 96, 350)]
+           (33, 2000, 1000), (67, 300, 513), (200, 100, 2000), (512, 96, 350),
+           # both sides of the lines up to which the rows are quantised inside the product
+           (16, 40, 4096), (17, 40, 4096), (64, 48, 1024), (65, 48, 512), (16, 4096, 4096), (16, 4112, 4096), (1, 7, 65537)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
