@@ -198,9 +198,9 @@ int emb_mx4_linear_grad(const void* dy, int32_t type, int64_t m, int64_t n, int6
   if (workspace_bytes < need) return EMB_ENOMEM;
   uint8_t* rows = static_cast<uint8_t*>(workspace);
   uint8_t* columns = need ? rows + align_up((size_t)Mx4(nullptr, m, n).bytes()) : nullptr;
-  int st = emb_mx4_quantize(dy, type, m, n, ldy, rows, columns, rounding, seed, step, stream);
-  if (st == EMB_OK) st = emb_mx4_matmul(rows, w_columns, m, k, n, dx, type, ldx, stream);
-  return st != EMB_OK ? st : emb_mx4_matmul(columns, saved, n, k, m, dw, dw_type, ldw, stream);
+  const int st = emb_mx4_quantize(dy, type, m, n, ldy, rows, columns, rounding, seed, step, stream);
+  if (st != EMB_OK) return st;
+  return status(launch_two_products(rows, w_columns, m, k, n, dx, type, ldx, columns, saved, n, k, m, dw, dw_type, ldw, S(stream)));
 }
 
 int emb_adamw_query_sizes(const emb_adamw_config* cfg, emb_adamw_sizes* out) {

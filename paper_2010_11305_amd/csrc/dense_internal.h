@@ -54,6 +54,10 @@ hipError_t launch_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* cod
 
 hipError_t launch_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k, void* c, int type, int64_t ldc,
                          hipStream_t s);
+// c1 = a1 b1^T and c2 = a2 b2^T (an empty one is left out), in one launch where both are small
+hipError_t launch_two_products(const void* a1, const void* b1, int64_t m1, int64_t n1, int64_t k1, void* c1, int type1,
+                               int64_t ldc1, const void* a2, const void* b2, int64_t m2, int64_t n2, int64_t k2, void* c2,
+                               int type2, int64_t ldc2, hipStream_t s);
 size_t linear_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                          int64_t ldy, void* workspace, hipStream_t s);

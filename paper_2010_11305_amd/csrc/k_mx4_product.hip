@@ -130,10 +130,15 @@ template <int FM>
 constexpr bool kStays = FM == 8;
 constexpr int kResident = 256;   // workgroups that stay: one to a CU
 
-// A workgroup of 2 x 2 waves computes (32 FM) x (32 FM) of C, a wave FM x FM tiles of 16 x 16.
+template <int FM>
+using Stages = v4i[kStages][4 * FM][64];     // codes, row tiles of both operands
+template <int FM>
+using StageScales = uint32_t[2][4 * FM][64];
+
+// Workgroup `block` of `blocks`, of 2 x 2 waves, computes (32 FM) x (32 FM) of C, a wave FM x FM tiles of 16 x 16.
 template <int TYPE, int FM>
-__global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
-                                                                 typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
+__device__ __forceinline__ void product(Stages<FM>& stage, StageScales<FM>& scales, v4i* leave, const Mx4& a, const Mx4& b,
+                                        typename Elem<TYPE>::type* __restrict__ c, int64_t ldc, uint32_t block, uint32_t blocks) {
   constexpr int kSide = 2 * FM;                       // row tiles of an operand in a stage
   constexpr int kTiles = 2 * kSide;
   constexpr int kLoads = kTiles / 4;                  // a wave's share of them, all of one operand
@@ -143,9 +148,6 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
   constexpr int kBytes = Elem<TYPE>::kBytes;
   constexpr int kOutCols = FM * 16 * kBytes <= 256 ? FM * 16 : 256 / kBytes;
   constexpr int kLanes = kOutCols * kBytes / 16, kRows = 64 / kLanes;   // lanes a row, rows an access
-  __shared__ v4i stage[kStages][kTiles][64];
-  __shared__ uint32_t scales[2][kTiles][64];
-  __shared__ v4i leave[kStays<FM> ? 4 : 1][kStays<FM> ? 256 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
@@ -153,10 +155,10 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
   // its L2 holds is used by the workgroups that run there together.
   // Their number is below 2^31.
   const uint32_t mt_all = (uint32_t)((a.row_tiles + kSide - 1) / kSide), nt_all = (uint32_t)((b.row_tiles + kSide - 1) / kSide);
-  const uint32_t total = mt_all * nt_all, xcd = blockIdx.x % 8;
+  const uint32_t total = mt_all * nt_all, xcd = block % 8;
   const uint32_t run0 = xcd * (total / 8) + (xcd < total % 8 ? xcd : total % 8);
   const uint32_t run = total / 8 + (xcd < total % 8 ? 1 : 0);
-  const uint32_t stride = (gridDim.x + 7) / 8;
+  const uint32_t stride = (blocks + 7) / 8;
   const auto place = [&](uint32_t nth, int64_t* rt_a, int64_t* rt_b) {
     const uint32_t id = run0 + nth, band = id / (8 * nt_all), in_band = id % (8 * nt_all);
     const uint32_t band_rows = mt_all - band * 8 < 8 ? mt_all - band * 8 : 8;
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
       load_to_lds(scales_at + parity * (kTiles * 256) + i * 1024, scale_at[i], scale_srd, k * kScaleBytes);
   };
 
-  uint32_t nth = blockIdx.x / 8;
+  uint32_t nth = block / 8;
   int64_t rt_a, rt_b;
   place(nth, &rt_a, &rt_b);
   aim(rt_a, rt_b);
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
     int l = lane;
     asm volatile("" : "+v"(l));  // or the addresses below would be computed ahead of all tiles, and kept
     if (row0 + FM * 16 <= a.rows && col0 + FM * 16 <= b.rows) {
-      uint8_t* own = kStays<FM> ? reinterpret_cast<uint8_t*>(&leave[kStays<FM> ? wave : 0][0])
+      uint8_t* own = kStays<FM> ? reinterpret_cast<uint8_t*>(leave + wave * 256)
                                 : reinterpret_cast<uint8_t*>(&stage[0][0][0]) + wave * 4096;
       typename Elem<TYPE>::type* out = c + (row0 + l / kLanes) * ldc + col0 + l % kLanes * (16 / kBytes);
 #pragma unroll
@@ -322,6 +324,28 @@ __global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
       for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   if (kStays<FM>) stage_ready<0>();  // no load to LDS outlives the workgroup
+}
+
+template <int TYPE, int FM>
+__global__ __launch_bounds__(256, FM == 8 ? 1 : 2) void k_product(Mx4 a, Mx4 b,
+                                                                 typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
+  __shared__ Stages<FM> stage;
+  __shared__ StageScales<FM> scales;
+  __shared__ v4i leave[kStays<FM> ? 4 * 256 : 1];
+  product<TYPE, FM>(stage, scales, leave, a, b, c, ldc, blockIdx.x, gridDim.x);
+}
+
+// Two products in one launch: the first `blocks1` workgroups compute c1, the others c2.
+template <int TYPE1, int TYPE2>
+__global__ __launch_bounds__(256, 2) void k_two_products(Mx4 a1, Mx4 b1, typename Elem<TYPE1>::type* __restrict__ c1,
+                                                         int64_t ldc1, uint32_t blocks1, Mx4 a2, Mx4 b2,
+                                                         typename Elem<TYPE2>::type* __restrict__ c2, int64_t ldc2) {
+  __shared__ Stages<2> stage;
+  __shared__ StageScales<2> scales;
+  if (blockIdx.x < blocks1)
+    product<TYPE1, 2>(stage, scales, nullptr, a1, b1, c1, ldc1, blockIdx.x, blocks1);
+  else
+    product<TYPE2, 2>(stage, scales, nullptr, a2, b2, c2, ldc2, blockIdx.x - blocks1, gridDim.x - blocks1);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -514,6 +538,36 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
   return hipGetLastError();
 }
 
+// Two products in one launch of 64 x 64 tiles: a launch saved, and the one fills the CUs that the other leaves.  It
+// loses where tiles of 256 or many waves along a long axis are worth more.  us of a layer's gradients (quantisation
+// included, replayed from a graph), together / one by one: 256x512x416 7.2 / 11.9, 2048x512x416 10.0 / 11.2 (of a
+// call 13.9 / 17.5), 2048x2048x512 15.5 / 18.6, 2048x2048x2048 (2048 tiles) 28.5 / 29.4, 4096x4096x512 (32 steps)
+// 38.2 / 40.9; past the lines 4096x2048x2048 45.5 / 42.9, 5000x512x416 (40 steps) 16.8 / 15.6, 16384x64x64 28.1 / 23.2.
+constexpr int64_t kTogetherTiles = 2048;  // of both
+constexpr int64_t kTogetherSteps = 32;    // column tiles of either
+bool together(const Mx4& a1, const Mx4& b1, const Mx4& a2, const Mx4& b2) {
+  return tiles_of(a1, b1, 2) + tiles_of(a2, b2, 2) <= kTogetherTiles && a1.col_tiles <= kTogetherSteps &&
+         a2.col_tiles <= kTogetherSteps;
+}
+
+template <int TYPE1, int TYPE2>
+hipError_t two_as(const Mx4& a1, const Mx4& b1, void* c1, int64_t ldc1, const Mx4& a2, const Mx4& b2, void* c2, int64_t ldc2,
+                  hipStream_t s) {
+  const int64_t t1 = tiles_of(a1, b1, 2), t2 = tiles_of(a2, b2, 2);
+  k_two_products<TYPE1, TYPE2><<<(unsigned)(t1 + t2), 256, 0, s>>>(
+      a1, b1, static_cast<typename Elem<TYPE1>::type*>(c1), ldc1, (uint32_t)t1, a2, b2,
+      static_cast<typename Elem<TYPE2>::type*>(c2), ldc2);
+  return hipGetLastError();
+}
+
+template <int TYPE1>
+hipError_t two_first(const Mx4& a1, const Mx4& b1, void* c1, int64_t ldc1, const Mx4& a2, const Mx4& b2, void* c2, int type2,
+                     int64_t ldc2, hipStream_t s) {
+  if (type2 == EMB_TYPE_FP32) return two_as<TYPE1, EMB_TYPE_FP32>(a1, b1, c1, ldc1, a2, b2, c2, ldc2, s);
+  if (type2 == EMB_TYPE_BF16) return two_as<TYPE1, EMB_TYPE_BF16>(a1, b1, c1, ldc1, a2, b2, c2, ldc2, s);
+  return two_as<TYPE1, EMB_TYPE_FP16>(a1, b1, c1, ldc1, a2, b2, c2, ldc2, s);
+}
+
 // Rows that every workgroup of k_skinny quantises by itself: few values, and not too many workgroups that do.  It saves
 // a launch.  us among other calls, with the quantisation inside / as a launch of its own: 16 rows, 4096 x 4096
 // 7.3 / 12.1; 4 rows, 4096 x 12800 9.3 / 11.9; 64 rows, 1000 x 1000 8.3 / 12.1, 8192 x 512 10.7 / 12.1; past the line
@@ -531,6 +585,20 @@ hipError_t launch_matmul(const void* a, const void* b, int64_t m, int64_t n, int
   if (type == EMB_TYPE_FP32) return matmul_as<EMB_TYPE_FP32>(a, b, m, n, k, c, ldc, s);
   if (type == EMB_TYPE_BF16) return matmul_as<EMB_TYPE_BF16>(a, b, m, n, k, c, ldc, s);
   return matmul_as<EMB_TYPE_FP16>(a, b, m, n, k, c, ldc, s);
+}
+
+hipError_t launch_two_products(const void* a1, const void* b1, int64_t m1, int64_t n1, int64_t k1, void* c1, int type1,
+                               int64_t ldc1, const void* a2, const void* b2, int64_t m2, int64_t n2, int64_t k2, void* c2,
+                               int type2, int64_t ldc2, hipStream_t s) {
+  const Mx4 qa1(a1, m1, k1), qb1(b1, n1, k1), qa2(a2, m2, k2), qb2(b2, n2, k2);
+  if (m1 && n1 && k1 && m2 && n2 && k2 && together(qa1, qb1, qa2, qb2)) {
+    if (type1 == EMB_TYPE_FP32) return two_first<EMB_TYPE_FP32>(qa1, qb1, c1, ldc1, qa2, qb2, c2, type2, ldc2, s);
+    if (type1 == EMB_TYPE_BF16) return two_first<EMB_TYPE_BF16>(qa1, qb1, c1, ldc1, qa2, qb2, c2, type2, ldc2, s);
+    return two_first<EMB_TYPE_FP16>(qa1, qb1, c1, ldc1, qa2, qb2, c2, type2, ldc2, s);
+  }
+  hipError_t e = m1 && n1 ? launch_matmul(a1, b1, m1, n1, k1, c1, type1, ldc1, s) : hipSuccess;
+  if (e == hipSuccess && m2 && n2) e = launch_matmul(a2, b2, m2, n2, k2, c2, type2, ldc2, s);
+  return e;
 }
 
 size_t linear_workspace(int64_t m, int64_t n, int64_t k) {

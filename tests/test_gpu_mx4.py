@@ -269,6 +269,33 @@ def test_layer_gradients_match_the_formula(torch, m, n, k):
         assert (np.abs(plain(got) - want) <= bound).all()
 
 
+@pytest.mark.parametrize("dw_dtype", DTYPES)
+@pytest.mark.parametrize("dy_dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (2, 500, 33), (65, 64, 129), (300, 200, 70), (700, 129, 513),
+                                   (4100, 40, 33), (90, 4100, 40)])
+def test_layer_gradients_of_every_type(torch, m, n, k, dy_dtype, dw_dtype):
+    """Both products by one launch, and (over more than 4096 rows or outputs) by one each."""
+    from paper_2010_11305_amd import mx4
+
+    print("gradients", m, n, k, dy_dtype, dw_dtype, flush=True)
+    x = matrix(torch, m, k, "float32", m + k) * (2.0**-12 / m**0.5)
+    w = matrix(torch, n, k, "float32", n + k) * (2.0**-12 / n**0.5)
+    dy = matrix(torch, m, n + 5, dy_dtype, m * n)[:, 1:n + 1]
+    layer = mx4.Linear(n, k, seed=6)
+    layer.load(w)
+    _, saved = layer.forward_train(x)
+    dx, dw = layer.backward(dy, saved, step=2, weight_grad_dtype=getattr(torch, dw_dtype))
+    D = plain(dy)
+    sr = dict(rounding="stochastic", seed=6, step=2)
+    rt = ref.mx4_round_trip
+    for got, a, b, dtype in ((dx, rt(D, **sr), rt(plain(w).T), dy_dtype), (dw, rt(D.T, tag=1, **sr), rt(plain(x).T), dw_dtype)):
+        assert got.dtype == getattr(torch, dtype)
+        want, bound = product_bound(a, b, dtype)
+        assert (np.abs(plain(got) - want) <= bound + (2.0**-24 if dtype == "float16" else 0)).all()
+    again = layer.backward(dy, saved, step=2, weight_grad_dtype=getattr(torch, dw_dtype))
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
 def test_layer_gradients_match_differences(torch):
     """On values that 4 bits hold exactly along both axes the layer is an exact linear map, and differences
     of sum(dy * y) are its gradients to the last bit: every term is a multiple of 1/8 below 2^15."""
