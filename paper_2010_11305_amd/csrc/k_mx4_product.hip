@@ -3,7 +3,7 @@
 // an MX4 matrix holds lane by lane.  Codes and scales go from memory to the instruction as they lie.
 //
 // k_product: tiles of C of 256, 128 or 64 rows and columns, the operands staged in LDS.  16384 x 8192 x 12800: 642 to
-// 740 us from card to card, 5.4 to 4.6 PFLOP/s.  The bound is power: on normal values the clock falls from 2.4 to
+// 770 us from card to card, 5.4 to 4.5 PFLOP/s.  The bound is power: on normal values the clock falls from 2.4 to
 // 1.6 GHz (560 us and 2.4 GHz on zeros, where a step takes 1190 cycles of the 1024 that its instructions issue for).
 // The 32x32x64 instruction needs 6% fewer cycles and takes 2% longer.
 // k_skinny: few rows against a weight that is read once.  1 row, 4096 x 12800: 5.3 us for 27.9 MB, much of it
