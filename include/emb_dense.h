@@ -20,7 +20,11 @@
  * compared with 16 random bits u: up when u * 2^-16 is less.  They are bits
  * 16 (j mod 2) .. +15 of word j div 2, j = column mod 8, of the Philox4x32-10 block
  * with key `seed` and counter (column div 8, row, step, 0), or (..., 1) for a matrix
- * quantised along its columns, whose rows and columns here are those of the result.
+ * quantised along its columns, whose rows and columns here are those of the result;
+ * (..., 2) and (..., 3) for the rows of emb_mx4_linear_train.  Matrices that meet in a product,
+ * or of which one follows from the other, must not draw the same bits: the expectation of the product
+ * of their roundings is then not that of their values.  So each of them has a seed or a step of its own; a
+ * weight takes another seed than the calls of its layer do.
  * A block that holds a NaN or an infinity has byte 255 and codes 0, and stands for NaN.
  *
  * An MX4 matrix [rows][cols] is one device buffer of emb_mx4_query_bytes, 256-byte
@@ -90,7 +94,8 @@ int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ld
  *
  * emb_mx4_linear_train: y [m][n] = Q(x) w^T with w by rows, and `saved`, the MX4 matrix [k][m] of
  * the transpose of x that the backward pass needs (emb_mx4_query_bytes(k, m)); x rounds as
- * `rounding` says (seed and step when stochastic).  y in the type of x.
+ * `rounding` says (seed and step when stochastic, its draws apart from those of the output gradient under
+ * the same seed and step).  y in the type of x.
  *
  * emb_mx4_linear_grad: for an output gradient dy [m][n], rounded as `rounding` says,
  *   dx [m][k] = Q(dy) Q(w^T)^T   in the type of dy, w_columns the MX4 matrix [k][n] of w^T

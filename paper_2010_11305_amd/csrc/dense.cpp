@@ -95,6 +95,15 @@ int plan_adamw(const emb_adamw_config* c, AdamPlan* p) {
   return EMB_OK;
 }
 
+int quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
+             int32_t rounding, uint64_t seed, uint32_t step, Mx4Stream draws, void* stream) {
+  if (!type_ok(type) || !rounding_ok(rounding) || !dims_ok(rows, cols) || !dims_ok(cols, rows)) return EMB_EINVAL;
+  if (rows == 0 || cols == 0) return EMB_OK;
+  if (!matrix_ok(x, type, rows, cols, ld) || (!by_rows && !by_columns)) return EMB_EINVAL;
+  if (!aligned(by_rows) || !aligned(by_columns)) return EMB_EINVAL;
+  return status(launch_quantize(x, type, rows, cols, ld, by_rows, by_columns, rounding, seed, step, draws, S(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -107,11 +116,7 @@ int emb_mx4_query_bytes(int64_t rows, int64_t cols, size_t* bytes) {
 
 int emb_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, void* by_rows,
                      void* by_columns, int32_t rounding, uint64_t seed, uint32_t step, void* stream) {
-  if (!type_ok(type) || !rounding_ok(rounding) || !dims_ok(rows, cols) || !dims_ok(cols, rows)) return EMB_EINVAL;
-  if (rows == 0 || cols == 0) return EMB_OK;
-  if (!matrix_ok(x, type, rows, cols, ld) || (!by_rows && !by_columns)) return EMB_EINVAL;
-  if (!aligned(by_rows) || !aligned(by_columns)) return EMB_EINVAL;
-  return status(launch_quantize(x, type, rows, cols, ld, by_rows, by_columns, rounding, seed, step, S(stream)));
+  return quantize(x, type, rows, cols, ld, by_rows, by_columns, rounding, seed, step, kStreamMatrix, stream);
 }
 
 int emb_mx4_dequantize(const void* q, int64_t rows, int64_t cols, void* x, int32_t type, int64_t ld, void* stream) {
@@ -176,7 +181,7 @@ int emb_mx4_linear_train(const void* x, int32_t type, int64_t m, int64_t k, int6
   if (need && (!workspace || !aligned(workspace) || !saved)) return EMB_EINVAL;
   if (m && n && (!type_ok(type) || !matrix_ok(y, type, m, n, ldy) || (k && (!w || !aligned(w))))) return EMB_EINVAL;
   if (workspace_bytes < need) return EMB_ENOMEM;
-  const int st = emb_mx4_quantize(x, type, m, k, ldx, workspace, saved, rounding, seed, step, stream);
+  const int st = quantize(x, type, m, k, ldx, workspace, saved, rounding, seed, step, kStreamTrainRows, stream);
   return st != EMB_OK ? st : emb_mx4_matmul(workspace, w, m, n, k, y, type, ldy, stream);
 }
 
@@ -198,7 +203,7 @@ int emb_mx4_linear_grad(const void* dy, int32_t type, int64_t m, int64_t n, int6
   if (workspace_bytes < need) return EMB_ENOMEM;
   uint8_t* rows = static_cast<uint8_t*>(workspace);
   uint8_t* columns = need ? rows + align_up((size_t)Mx4(nullptr, m, n).bytes()) : nullptr;
-  const int st = emb_mx4_quantize(dy, type, m, n, ldy, rows, columns, rounding, seed, step, stream);
+  const int st = quantize(dy, type, m, n, ldy, rows, columns, rounding, seed, step, kStreamMatrix, stream);
   if (st != EMB_OK) return st;
   return status(launch_two_products(rows, w_columns, m, k, n, dx, type, ldx, columns, saved, n, k, m, dw, dw_type, ldw, S(stream)));
 }

@@ -46,8 +46,11 @@ constexpr int64_t kMaxDepth = (int64_t)1 << 24;  // columns of a product's opera
 // no device memory holds a matrix of more bytes; the tile counts of smaller ones fit a grid
 constexpr double kMaxBytes = (double)((int64_t)1 << 40);
 
+// Last word of the random counter of a matrix quantised by rows; by columns it is the next one.
+enum Mx4Stream : uint32_t { kStreamMatrix = 0, kStreamTrainRows = 2 };
+
 hipError_t launch_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t ld, void* by_rows,
-                           void* by_columns, int rounding, uint64_t seed, uint32_t step, hipStream_t s);
+                           void* by_columns, int rounding, uint64_t seed, uint32_t step, Mx4Stream stream, hipStream_t s);
 hipError_t launch_dequantize(const void* q, int64_t rows, int64_t cols, void* x, int type, int64_t ld, hipStream_t s);
 hipError_t launch_pack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* q, hipStream_t s);
 hipError_t launch_unpack(const void* q, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, hipStream_t s);

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
 #pragma unroll
     for (int j = 0; j < kBlock; ++j) r.put(j, load_bits<TYPE>(&stage[j * kPitch + c]));
     Mx4Random q = rnd;
-    q.tag = 1;
+    q.tag += 1;
     const uint4 code = quantize_block<TYPE, STOCHASTIC>(r, (uint32_t)(row0 / 8), (uint32_t)col, q, &s);
     const int lane = (int)(row0 % kTileCols / kBlock) * 16 + (int)(col % kTileRows);
     *reinterpret_cast<uint4*>(by_columns + qc.tile(rt, kt) + 16 * lane) = code;
@@ -214,8 +214,8 @@ hipError_t quantize_as(const void* x, int64_t rows, int64_t cols, int64_t ld, vo
 }  // namespace
 
 hipError_t launch_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t ld, void* by_rows,
-                           void* by_columns, int rounding, uint64_t seed, uint32_t step, hipStream_t s) {
-  const Mx4Random rnd = {(uint32_t)seed, (uint32_t)(seed >> 32), step, 0};
+                           void* by_columns, int rounding, uint64_t seed, uint32_t step, Mx4Stream stream, hipStream_t s) {
+  const Mx4Random rnd = {(uint32_t)seed, (uint32_t)(seed >> 32), step, stream};
   const bool sr = rounding == EMB_ROUND_STOCHASTIC;
   switch (type) {
     case EMB_TYPE_FP32:

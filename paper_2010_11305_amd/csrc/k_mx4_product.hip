@@ -617,7 +617,7 @@ hipError_t launch_linear(const void* x, int type, int64_t m, int64_t k, int64_t 
     return skinny<EMB_TYPE_FP16, EMB_TYPE_FP16, false>(qw, qx, full, static_cast<uint16_t*>(y), ldy, s);
   }
   if (k) {
-    const hipError_t e = launch_quantize(x, type, m, k, ldx, workspace, nullptr, EMB_ROUND_NEAREST, 0, 0, s);
+    const hipError_t e = launch_quantize(x, type, m, k, ldx, workspace, nullptr, EMB_ROUND_NEAREST, 0, 0, kStreamMatrix, s);
     if (e != hipSuccess) return e;
   }
   return launch_matmul(workspace, w, m, n, k, y, type, ldy, s);

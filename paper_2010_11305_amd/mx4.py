@@ -159,9 +159,11 @@ class Linear:
     """The products of a linear layer y = x w^T in 4 bits, forward and backward.
 
     The full-precision weight stays with the caller (and its optimizer); load() brings it
-    here in 4 bits along both axes, after every update.  Rows and weights round as
+    here in 4 bits along both axes, after every update.  Rows (of forward_train) and weights round as
     `rounding` says, output gradients as `grad_rounding` does: stochastic rounding keeps
-    gradients unbiased.
+    gradients unbiased.  Weights, rows and output gradients draw from streams of their own; pass the
+    number of the training step as `step`, or every step draws the same bits, and give each layer
+    its own seed.
 
         y  = Q(x) Q(w)^T
         dx = Q(dy) Q(w^T)^T        blocks along the outputs
@@ -173,12 +175,13 @@ class Linear:
         lib.rounding_of(rounding), lib.rounding_of(grad_rounding)
         self.out_features, self.in_features = out_features, in_features
         self.rounding, self.grad_rounding, self.seed = rounding, grad_rounding, seed
+        self.weight_seed = seed ^ 1 << 63    # the calls of the library separate rows and output gradients, not the weight
         self.by_rows = Mx4Matrix(out_features, in_features, device)
         self.by_columns = Mx4Matrix(in_features, out_features, device)
 
     def load(self, weight, step=0):
         """weight [out_features, in_features], full precision."""
-        quantize_both(weight, self.rounding, self.seed, step, (self.by_rows, self.by_columns))
+        quantize_both(weight, self.rounding, self.weight_seed, step, (self.by_rows, self.by_columns))
 
     def forward(self, x):
         return linear(x, self.by_rows)
