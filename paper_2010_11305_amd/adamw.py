@@ -20,7 +20,8 @@ dtype_of = attrgetter("dtype")
 
 
 class AdamW:
-    """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous.
+    """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous.  A parameter may be given other
+    memory later (through `data`), of the same type, device and size.
     weight_decay: one number, or one per tensor.  grad_dtype: the type of the gradients (default:
     that of the parameters)."""
 
@@ -32,11 +33,9 @@ class AdamW:
         p0 = self.params[0]
         self.dtype, self.device = p0.dtype, p0.device
         self.grad_dtype = grad_dtype or self.dtype
-        for p in self.params:
-            if p.dtype != self.dtype or p.device != self.device or not p.is_cuda or not p.is_contiguous():
-                raise ValueError("params must be contiguous tensors of one type on one GPU")
         n = len(self.params)
         self.sizes = [p.numel() for p in self.params]
+        self._hold()
         self.lr, self.state_bits = float(lr), state_bits
         c = lib.AdamwConfig()
         self._sizes = (ctypes.c_int64 * n)(*self.sizes)
@@ -60,6 +59,18 @@ class AdamW:
             lib.check(L.emb_adamw_create(ctypes.byref(c), self.state_buffer.data_ptr(), self._layout.state_bytes,
                                          torch.cuda.current_stream().cuda_stream, ctypes.byref(self._h)),
                       "emb_adamw_create")
+
+    def _hold(self):
+        """Check the parameters and keep their memory by views of it: as long as a parameter's address is that of its
+        view, nothing else can have come to lie there, and step() need not look at type, device and size again."""
+        for p, size in zip(self.params, self.sizes):
+            if (p.dtype != self.dtype or p.device != self.device or not p.is_cuda or not p.is_contiguous()
+                    or p.numel() != size):
+                raise ValueError("params must be contiguous tensors of one type on one GPU, and keep type, device and size")
+        self._held = [p.detach() for p in self.params]
+        self._pointers = array("Q", map(Tensor.data_ptr, self._held))
+        # a tensor of one dimension and the same elements cannot lie otherwise
+        self._wide = [p for p in self.params if p.dim() > 1]
 
     def close(self):
         if getattr(self, "_h", None):
@@ -93,6 +104,8 @@ class AdamW:
                 raise ValueError(f"grad_scale must be one float32 value on {self.device}")
             scale = grad_scale.data_ptr()
         pp = array("Q", map(Tensor.data_ptr, self.params))
+        if pp != self._pointers or not all(map(Tensor.is_contiguous, self._wide)):
+            self._hold()   # another storage, as a parameter's `data` may be given
         gp = array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
         lib.call("emb_adamw_step", self.device, self._h, pp.buffer_info()[0], gp.buffer_info()[0],
                  self.lr if lr is None else float(lr), scale)

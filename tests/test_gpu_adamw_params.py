@@ -1,0 +1,64 @@
+"""Parameters of AdamW whose memory or type changes between steps."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    if not t.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2010_11305_amd import dense_lib
+    dense_lib.load()
+    return t
+
+
+def make(torch, **kw):
+    from paper_2010_11305_amd.adamw import AdamW
+
+    params = [torch.nn.Parameter(torch.randn(s, device="cuda")) for s in ((7,), (40, 30), (33,))]
+    return params, AdamW(params, lr=1e-2, grad_dtype=torch.bfloat16, **kw)
+
+
+def grads_of(torch, params):
+    return [torch.ones(p.shape, dtype=torch.bfloat16, device="cuda") for p in params]
+
+
+@pytest.mark.parametrize("change", ["type", "half type", "size", "order", "device"])
+def test_a_changed_parameter_is_refused(torch, change):
+    """Gradients still fit (they have a type of their own); the parameter no longer does, and nothing is written."""
+    params, opt = make(torch)
+    opt.step(grads_of(torch, params))
+    p = params[1]
+    grads = grads_of(torch, params)
+    if change == "type":
+        p.data = p.data.bfloat16()
+    elif change == "half type":
+        p.data = p.data.half()
+    elif change == "size":
+        p.data = torch.zeros(20, 30, device="cuda")
+    elif change == "order":
+        p.data = p.data.t()
+    else:
+        p.data = p.data.cpu()
+    before = [q.detach().clone() for q in params]
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            opt.step(grads)
+    assert opt.step_count == 1 and all(torch.equal(a, b) for a, b in zip(before, params))
+
+
+def test_other_memory_of_the_same_kind_is_taken(torch):
+    params, opt = make(torch)
+    other, same = make(torch)
+    for p, q in zip(params, other):
+        q.data.copy_(p.data)
+    for step in range(3):
+        if step:
+            params[1].data = params[1].data.clone()
+        old = params[1].data
+        opt.step(grads_of(torch, params))
+        same.step(grads_of(torch, other))
+        assert all(torch.equal(p, q) for p, q in zip(params, other))
+        assert params[1].data_ptr() == old.data_ptr()
