@@ -20,8 +20,8 @@ dtype_of = attrgetter("dtype")
 
 
 class AdamW:
-    """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous.  A parameter may be given other
-    memory later (through `data`), of the same type, device and size.
+    """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous, none sharing memory with
+    another.  A parameter may be given other memory later (through `data`), of the same type, device and size.
     weight_decay: one number, or one per tensor.  grad_dtype: the type of the gradients (default:
     that of the parameters)."""
 
@@ -67,6 +67,11 @@ class AdamW:
             if (p.dtype != self.dtype or p.device != self.device or not p.is_cuda or not p.is_contiguous()
                     or p.numel() != size):
                 raise ValueError("params must be contiguous tensors of one type on one GPU, and keep type, device and size")
+        end = 0
+        for start, size in sorted((p.data_ptr(), p.numel() * p.element_size()) for p in self.params if p.numel()):
+            if start < end:
+                raise ValueError("params must not share memory (a tied parameter is given once)")
+            end = start + size
         self._held = [p.detach() for p in self.params]
         self._pointers = array("Q", map(Tensor.data_ptr, self._held))
         # a tensor of one dimension and the same elements cannot lie otherwise

@@ -62,3 +62,20 @@ def test_other_memory_of_the_same_kind_is_taken(torch):
         same.step(grads_of(torch, other))
         assert all(torch.equal(p, q) for p, q in zip(params, other))
         assert params[1].data_ptr() == old.data_ptr()
+
+
+def test_shared_memory_is_refused(torch):
+    """Two tensors in one memory would be updated by two workgroups at once."""
+    from paper_2010_11305_amd.adamw import AdamW
+
+    base = torch.zeros(100, device="cuda")
+    p, other = torch.zeros(10, device="cuda"), torch.zeros(64, device="cuda")
+    for bad in ([p, other, p], [base[:51], p, base[50:]], [base, base[10:20].view(5, 2)]):
+        with pytest.raises(ValueError):
+            AdamW(bad)
+    params = [base[:50], base[50:], p]
+    opt = AdamW(params + [base[7:7]])
+    params[2].data = base[20:30]
+    with pytest.raises(ValueError):
+        opt.step([torch.ones(n, device="cuda") for n in (50, 50, 10, 0)])
+    assert (base == 0).all()
