@@ -135,7 +135,8 @@ int emb_mx4_linear_grad(const void* dy, int32_t type, int64_t m, int64_t n, int6
  * Philox4x32-10 block with key `seed` and counter (low and high half of i div 4, t, 0),
  * the low half of w rounds m (up when its share of 2^16 is below the value's share of
  * the step between two neighbours), the high half r, and their exclusive or the
- * parameter.  Nearest rounding of slowly moving moments loses their small changes;
+ * parameter.  The first elements share these blocks with row 0 of an MX4 matrix under the same
+ * seed and step: a model's optimizer and its layers have different seeds.  Nearest rounding of slowly moving moments loses their small changes;
  * stochastic rounding keeps them on average.
  *
  *   sizes[t]       elements of tensor t, >= 0

@@ -22,6 +22,7 @@ dtype_of = attrgetter("dtype")
 class AdamW:
     """params: float32 or bfloat16 tensors on one GPU, all of one type, contiguous, none sharing memory with
     another.  A parameter may be given other memory later (through `data`), of the same type, device and size.
+    seed: of stochastic rounding, another one than those of the model's 4-bit layers.
     weight_decay: one number, or one per tensor.  grad_dtype: the type of the gradients (default:
     that of the parameters)."""
 
@@ -36,7 +37,7 @@ class AdamW:
         n = len(self.params)
         self.sizes = [p.numel() for p in self.params]
         self._hold()
-        self.lr, self.state_bits = float(lr), state_bits
+        self.lr, self.state_bits, self.seed = float(lr), state_bits, int(seed)
         c = lib.AdamwConfig()
         self._sizes = (ctypes.c_int64 * n)(*self.sizes)
         c.num_tensors, c.param_type, c.sizes = n, lib.type_of(self.dtype), self._sizes
@@ -49,7 +50,7 @@ class AdamW:
             self._decays = (ctypes.c_double * n)(*weight_decay)
             c.weight_decays = self._decays
         c.grad_type, c.state_bits, c.rounding = lib.type_of(self.grad_dtype), int(state_bits), lib.rounding_of(rounding)
-        c.beta1, c.beta2, c.eps, c.seed = float(betas[0]), float(betas[1]), float(eps), int(seed)
+        c.beta1, c.beta2, c.eps, c.seed = float(betas[0]), float(betas[1]), float(eps), self.seed
         L = lib.load()
         self._layout = lib.AdamwSizes()
         lib.check(L.emb_adamw_query_sizes(ctypes.byref(c), ctypes.byref(self._layout)), "emb_adamw_query_sizes")

@@ -45,7 +45,7 @@ class Tower:
                        for i, (k, n) in enumerate(zip(widths, widths[1:]))]
         params = [*self.weights, *self.biases, self.last]
         self.opt = adamw.AdamW(params, lr=lr, weight_decay=[0.01] * len(self.weights) + [0.0] * (len(self.biases) + 1),
-                               state_bits=state_bits, rounding="stochastic", seed=seed)
+                               state_bits=state_bits, rounding="stochastic", seed=seed + len(self.layers))
         self.load()
 
     def load(self):
