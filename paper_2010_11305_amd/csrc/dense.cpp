@@ -308,8 +308,10 @@ int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads,
       ptr.p[k] = k < n ? params[first + k] : nullptr;
       ptr.g[k] = k < n ? grads[first + k] : nullptr;
     }
-    const hipError_t e = launch_adamw(h->dev, ptr, (uint32_t)first, part0, parts, c, grad_scale, h->param_type,
-                                      h->grad_type, h->state_bits, h->rounding, S(stream));
+    const hipError_t e = in_launches(parts, kAdamThreads, [&](int64_t from, unsigned some) {
+      return launch_adamw(h->dev, ptr, (uint32_t)first, part0 + from, some, c, grad_scale, h->param_type, h->grad_type,
+                          h->state_bits, h->rounding, S(stream));
+    });
     if (e != hipSuccess) return EMB_EHIP;
   }
   h->step += 1;

@@ -6,6 +6,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "dense_launch.h"
 #include "emb_dense.h"
 
 namespace embd {
@@ -43,7 +44,7 @@ struct Mx4 {
 
 constexpr int64_t kMaxDim = (int64_t)1 << 31;  // rows and columns stay below it
 constexpr int64_t kMaxDepth = (int64_t)1 << 24;  // columns of a product's operands: offsets inside 8 row tiles fit 31 bits
-// no device memory holds a matrix of more bytes; the tile counts of smaller ones fit a grid
+// no device memory holds a matrix of more bytes; the tile counts of smaller ones fit 31 bits
 constexpr double kMaxBytes = (double)((int64_t)1 << 40);
 
 // Last word of the random counter of a matrix quantised by rows; by columns it is the next one.

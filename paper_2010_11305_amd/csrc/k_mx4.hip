@@ -28,35 +28,36 @@ __device__ __forceinline__ void store_scale(uint8_t* out, const Mx4& q, int64_t 
 template <int TYPE, bool BY_COLUMNS>
 struct Stage {
   static constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
-  static constexpr int kRows = kBlock;
+  static constexpr int kRows = kQuantizeRows;
   static constexpr int kThreads = 256;
   static constexpr int kPitch = kTileCols + kPiece;  // 16 more bytes a row: rows start in different banks
   // The scale bytes of four tiles along a quantised axis lie in one dword, and a column's codes of 128 rows in one
   // tile: where there are many workgroups those of 512 rows (by columns) x 512 columns run on one XCD, whose
   // L2 joins what they write.
-  static constexpr int kSquareRows = BY_COLUMNS ? 512 / kRows : 1;
-  static constexpr int kSquareCols = 4;
+  static constexpr int kSquareRows = square_rows(BY_COLUMNS);
   static constexpr int kSquare = kSquareRows * kSquareCols;
-  static constexpr int kSquaresFrom = 64;
 };
+static_assert(kQuantizeRows == kBlock && kQuantizeCols == kTileCols);
 
 template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
 __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::type* __restrict__ x, Mx4 qr, Mx4 qc,
                                                   int64_t ld, uint8_t* __restrict__ by_rows,
-                                                  uint8_t* __restrict__ by_columns, Mx4Random rnd) {
+                                                  uint8_t* __restrict__ by_columns, Mx4Random rnd, uint32_t first,
+                                                  uint32_t workgroups) {
   using E = typename Elem<TYPE>::type;
   using St = Stage<TYPE, BY_COLUMNS>;
   constexpr int kPiece = St::kPiece, kPitch = St::kPitch, kPieces = kTileCols / kPiece;
   __shared__ __attribute__((aligned(16))) E stage[St::kRows * kPitch];
-  const uint32_t wide = (uint32_t)((qr.cols + kTileCols * St::kSquareCols - 1) / (kTileCols * St::kSquareCols));
-  uint32_t square = blockIdx.x / St::kSquare, in = blockIdx.x % St::kSquare;
-  if (gridDim.x >= St::kSquaresFrom * St::kSquare) {  // workgroups go to the XCDs in turn
-    square = blockIdx.x / (8 * St::kSquare) * 8 + blockIdx.x % 8;
-    in = blockIdx.x / 8 % St::kSquare;
+  const uint32_t wide = (uint32_t)((qr.cols + kTileCols * kSquareCols - 1) / (kTileCols * kSquareCols));
+  const uint32_t block = first + blockIdx.x;
+  uint32_t square = block / St::kSquare, in = block % St::kSquare;
+  if (workgroups >= kSquaresFrom * St::kSquare) {  // workgroups go to the XCDs in turn
+    square = block / (8 * St::kSquare) * 8 + block % 8;
+    in = block / 8 % St::kSquare;
   }
   // counts of workgroups and tiles are below 2^31: divisions of 32 bits
-  const int64_t row0 = ((int64_t)(square / wide) * St::kSquareRows + in / St::kSquareCols) * St::kRows;
-  const int64_t kt0 = (int64_t)(square % wide) * St::kSquareCols + in % St::kSquareCols, col0 = kt0 * kTileCols;
+  const int64_t row0 = ((int64_t)(square / wide) * St::kSquareRows + in / kSquareCols) * St::kRows;
+  const int64_t kt0 = (int64_t)(square % wide) * kSquareCols + in % kSquareCols, col0 = kt0 * kTileCols;
   // by columns the rows go on to the end of their tile of 128
   const int64_t row_end = BY_COLUMNS ? qc.col_tiles * kTileCols : qr.row_tiles * kTileRows;
   if (row0 >= row_end || kt0 >= qr.col_tiles) return;
@@ -102,9 +103,10 @@ __global__ __launch_bounds__(256) void k_quantize(const typename Elem<TYPE>::typ
 // Expansion: a thread takes 8 values (one dword of codes), 16 consecutive threads one row of a
 // tile, so that a wave writes whole lines.
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::type* __restrict__ x, int64_t ld) {
-  const uint32_t wide = (uint32_t)q.col_tiles;
-  const int64_t rt = blockIdx.x / wide, kt = blockIdx.x % wide;
+__global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::type* __restrict__ x, int64_t ld,
+                                                    uint32_t first) {
+  const uint32_t wide = (uint32_t)q.col_tiles, tile = first + blockIdx.x;
+  const int64_t rt = tile / wide, kt = tile % wide;
   const int rr = threadIdx.x >> 4, c8 = threadIdx.x & 15, lane = (c8 >> 2) * 16 + rr;
   const int64_t row = rt * kTileRows + rr, col = kt * kTileCols + c8 * 8;
   if (row >= q.rows || col >= q.cols) return;
@@ -143,8 +145,8 @@ __global__ __launch_bounds__(256) void k_dequantize(Mx4 q, typename Elem<TYPE>::
 
 // Plain codes to tiles and back: a thread takes one block.
 __global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                              Mx4 q, uint8_t* __restrict__ out) {
-  const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
+                                              Mx4 q, uint8_t* __restrict__ out, uint32_t first) {
+  const uint32_t tile = (first + blockIdx.x) * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
   if (tile >= q.row_tiles * q.col_tiles) return;
   const int lane = threadIdx.x & 63;
   const int64_t rt = tile / wide, kt = tile % wide;
@@ -168,8 +170,9 @@ __global__ __launch_bounds__(256) void k_pack(const uint8_t* __restrict__ codes,
   store_scale(out, q, rt, kt, lane, n > 0 ? scales[row * blocks + col / kBlock] : 0u);
 }
 
-__global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
+__global__ __launch_bounds__(256) void k_unpack(Mx4 q, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                uint32_t first) {
+  const uint32_t tile = (first + blockIdx.x) * 4 + (threadIdx.x >> 6), wide = (uint32_t)q.col_tiles;
   if (tile >= q.row_tiles * q.col_tiles) return;
   const int lane = threadIdx.x & 63;
   const int64_t rt = tile / wide, kt = tile % wide;
@@ -194,13 +197,13 @@ template <int TYPE, bool STOCHASTIC, bool BY_ROWS, bool BY_COLUMNS>
 hipError_t quantize_along(const void* x, int64_t rows, int64_t cols, int64_t ld, void* by_rows, void* by_columns,
                           const Mx4Random& rnd, hipStream_t s) {
   using St = Stage<TYPE, BY_COLUMNS>;
-  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  const int64_t squares = up(rows, St::kRows * St::kSquareRows) * up(cols, kTileCols * St::kSquareCols);
-  const int64_t grid = (squares >= St::kSquaresFrom ? up(squares, 8) * 8 : squares) * St::kSquare;
-  k_quantize<TYPE, STOCHASTIC, BY_ROWS, BY_COLUMNS><<<(unsigned)grid, St::kThreads, 0, s>>>(
-      static_cast<const typename Elem<TYPE>::type*>(x), Mx4(by_rows, rows, cols), Mx4(by_columns, cols, rows), ld,
-      static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), rnd);
-  return hipGetLastError();
+  const int64_t workgroups = quantize_workgroups(rows, cols, BY_COLUMNS);
+  return in_launches(workgroups, St::kThreads, [&](int64_t first, unsigned n) {
+    k_quantize<TYPE, STOCHASTIC, BY_ROWS, BY_COLUMNS><<<n, St::kThreads, 0, s>>>(
+        static_cast<const typename Elem<TYPE>::type*>(x), Mx4(by_rows, rows, cols), Mx4(by_columns, cols, rows), ld,
+        static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), rnd, (uint32_t)first, (uint32_t)workgroups);
+    return hipGetLastError();
+  });
 }
 
 template <int TYPE, bool STOCHASTIC>
@@ -232,27 +235,33 @@ hipError_t launch_quantize(const void* x, int type, int64_t rows, int64_t cols, 
 
 hipError_t launch_dequantize(const void* qv, int64_t rows, int64_t cols, void* x, int type, int64_t ld, hipStream_t s) {
   const Mx4 q(qv, rows, cols);
-  const unsigned grid = (unsigned)(q.row_tiles * q.col_tiles);
-  if (type == EMB_TYPE_FP32)
-    k_dequantize<EMB_TYPE_FP32><<<grid, 256, 0, s>>>(q, static_cast<float*>(x), ld);
-  else if (type == EMB_TYPE_BF16)
-    k_dequantize<EMB_TYPE_BF16><<<grid, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld);
-  else
-    k_dequantize<EMB_TYPE_FP16><<<grid, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld);
-  return hipGetLastError();
+  return in_launches(q.row_tiles * q.col_tiles, 256, [&](int64_t first, unsigned n) {
+    const uint32_t f = (uint32_t)first;
+    if (type == EMB_TYPE_FP32)
+      k_dequantize<EMB_TYPE_FP32><<<n, 256, 0, s>>>(q, static_cast<float*>(x), ld, f);
+    else if (type == EMB_TYPE_BF16)
+      k_dequantize<EMB_TYPE_BF16><<<n, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld, f);
+    else
+      k_dequantize<EMB_TYPE_FP16><<<n, 256, 0, s>>>(q, static_cast<uint16_t*>(x), ld, f);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_pack(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* qv,
                        hipStream_t s) {
   const Mx4 q(qv, rows, cols);
-  k_pack<<<(unsigned)((q.row_tiles * q.col_tiles + 3) / 4), 256, 0, s>>>(codes, scales, q, static_cast<uint8_t*>(qv));
-  return hipGetLastError();
+  return in_launches(ceil_div(q.row_tiles * q.col_tiles, 4), 256, [&](int64_t first, unsigned n) {
+    k_pack<<<n, 256, 0, s>>>(codes, scales, q, static_cast<uint8_t*>(qv), (uint32_t)first);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_unpack(const void* qv, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
   const Mx4 q(qv, rows, cols);
-  k_unpack<<<(unsigned)((q.row_tiles * q.col_tiles + 3) / 4), 256, 0, s>>>(q, codes, scales);
-  return hipGetLastError();
+  return in_launches(ceil_div(q.row_tiles * q.col_tiles, 4), 256, [&](int64_t first, unsigned n) {
+    k_unpack<<<n, 256, 0, s>>>(q, codes, scales, (uint32_t)first);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace embd

@@ -364,13 +364,14 @@ struct FullRows {
 
 template <int XT, int TYPE, int MT, bool SWAP>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(Mx4 w, Mx4 x, FullRows full,
-                                                              typename Elem<TYPE>::type* __restrict__ c, int64_t ldc) {
+                                                              typename Elem<TYPE>::type* __restrict__ c, int64_t ldc,
+                                                              int64_t first) {
   constexpr bool kFused = XT >= 0;
   __shared__ f32x4 sums[kSkinnyWaves][MT][64];
   __shared__ uint4 codes[kFused ? kFusedValues / kBlock : 1];
   __shared__ uint32_t code_scales[kFused ? kFusedValues / kBlock / 4 : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t rt = blockIdx.x;
+  const int64_t rt = first + blockIdx.x;
   const int KT = (int)w.col_tiles, KG = (int)w.col_groups;
   const int64_t x_tile0 = (int64_t)blockIdx.y * MT;
   const int m = (int)(x.rows - x_tile0 * kTileRows < MT * kTileRows ? x.rows - x_tile0 * kTileRows : MT * kTileRows);
@@ -472,14 +473,16 @@ hipError_t skinny(const Mx4& w, const Mx4& x, const FullRows& full, typename Ele
   const int64_t need = (w.col_groups + rounds - 1) / rounds;
   const unsigned threads = 64u * (unsigned)(XT >= 0 && need < 4 ? 4 : need);
   const int mt = skinny_tiles(x.row_tiles);
-  const dim3 grid((unsigned)w.row_tiles, (unsigned)((x.row_tiles + mt - 1) / mt));
-  if (mt == 1)
-    k_skinny<XT, TYPE, 1, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
-  else if (mt == 2)
-    k_skinny<XT, TYPE, 2, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
-  else
-    k_skinny<XT, TYPE, 4, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc);
-  return hipGetLastError();
+  return in_launches(w.row_tiles, (int)threads, [&](int64_t first, unsigned n) {
+    const dim3 grid(n, (unsigned)ceil_div(x.row_tiles, mt));
+    if (mt == 1)
+      k_skinny<XT, TYPE, 1, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc, first);
+    else if (mt == 2)
+      k_skinny<XT, TYPE, 2, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc, first);
+    else
+      k_skinny<XT, TYPE, 4, SWAP><<<grid, threads, 0, s>>>(w, x, full, c, ldc, first);
+    return hipGetLastError();
+  });
 }
 
 // C = 0 (a product over no columns).
@@ -489,9 +492,7 @@ __global__ __launch_bounds__(256) void k_zero(int64_t m, int64_t n, typename Ele
 }
 
 // ---- the way of a product ------------------------------------------------------------------------
-int64_t tiles_of(const Mx4& a, const Mx4& b, int f) {
-  return ((a.row_tiles + 2 * f - 1) / (2 * f)) * ((b.row_tiles + 2 * f - 1) / (2 * f));
-}
+int64_t tiles_of(const Mx4& a, const Mx4& b, int f) { return product_tiles(a.row_tiles, b.row_tiles, f); }
 
 // k_skinny reads its w once for each 64 rows of x and its x once for each 16 rows of w, all of it from L2 at best: it
 // wins while its workgroups are about as many as the CUs can hold at once, whatever the columns, and for up
@@ -503,15 +504,6 @@ bool use_skinny(const Mx4& a, const Mx4& b) {
   const int64_t w = a.row_tiles < b.row_tiles ? b.row_tiles : a.row_tiles;
   const int mt = skinny_tiles(x);
   return x <= 1 || w * ((x + mt - 1) / mt) * (1 + mt) <= 1920;
-}
-
-// Row tiles of a wave's side in k_product, the side of a workgroup's tile being 32 of them: the least time, in
-// units of a round of 256 workgroups of 256 x 256.  Full rounds (16384x8192x12800): 92 us at f = 8, 28.7 at 4, 10.9
-// at 2; one round alone (1024x1024x12800, 256 CUs not full at 8 and 4): 63, 25 and 18.3.
-int tile_side(const Mx4& a, const Mx4& b) {
-  const auto rounds = [&](int f) { return (double)((tiles_of(a, b, f) + 255) / 256); };
-  const double t8 = rounds(8), t4 = 0.31 * rounds(4) + 0.09, t2 = 0.12 * (rounds(2) + 1);
-  return t8 <= t4 && t8 <= t2 ? 8 : t4 <= t2 ? 4 : 2;
 }
 
 template <int TYPE>
@@ -526,7 +518,7 @@ hipError_t matmul_as(const void* a, const void* b, int64_t m, int64_t n, int64_t
   if (use_skinny(qa, qb))
     return qb.row_tiles < qa.row_tiles ? skinny<-1, TYPE, true>(qa, qb, FullRows{}, c, ldc, s)
                                        : skinny<-1, TYPE, false>(qb, qa, FullRows{}, c, ldc, s);
-  const int f = tile_side(qa, qb);
+  const int f = product_side(qa.row_tiles, qb.row_tiles);
   const int64_t tiles = tiles_of(qa, qb, f);
   const unsigned grid = (unsigned)(f == 8 && tiles > kResident ? kResident : tiles);
   if (f == 8)
