@@ -85,7 +85,8 @@ int emb_mx4_matmul(const void* a, const void* b, int64_t m, int64_t n, int64_t k
  * ldx), quantised to nearest on the way, and an MX4 weight w [n][k]; y in the type of
  * x, row stride ldy.  Equal to emb_mx4_quantize of x and emb_mx4_matmul up to the order
  * of the FP32 sums.  workspace: emb_mx4_linear_workspace bytes, 256-byte aligned, or NULL
- * when that is 0.  Enqueue-only. */
+ * when that is 0: then y is written while x is still read, and must share no element with it.
+ * Enqueue-only. */
 int emb_mx4_linear_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
 int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ldx, const void* w, int64_t n, void* y,
                    int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);

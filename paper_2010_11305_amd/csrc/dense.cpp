@@ -38,6 +38,20 @@ bool matrix_ok(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t 
   return (double)rows * (double)ld * type_bytes(type) <= 4.0 * kMaxBytes;
 }
 
+// Whether two matrices share an element: by their extents, or, where their rows lie equally far apart, by the
+// columns that each takes of them.
+bool share_elements(const void* x, int64_t x_rows, int64_t x_cols, int64_t x_ld, const void* y, int64_t y_rows, int64_t y_cols,
+                    int64_t y_ld, int64_t bytes) {
+  if (!x_rows || !x_cols || !y_rows || !y_cols) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+  const uintptr_t a_end = a + (uintptr_t)(((x_rows - 1) * x_ld + x_cols) * bytes);
+  const uintptr_t b_end = b + (uintptr_t)(((y_rows - 1) * y_ld + y_cols) * bytes);
+  if (a_end <= b || b_end <= a) return false;
+  if (x_ld != y_ld) return true;
+  const uintptr_t row = (uintptr_t)(x_ld * bytes), behind = b >= a ? (b - a) % row : (row - (a - b) % row) % row;
+  return behind < (uintptr_t)(x_cols * bytes) || behind + (uintptr_t)(y_cols * bytes) > row;
+}
+
 }  // namespace
 
 struct emb_adamw {
@@ -164,6 +178,7 @@ int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ld
   const size_t need = k ? linear_workspace(m, n, k) : 0;
   if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
   if (workspace_bytes < need) return EMB_ENOMEM;
+  if (k && !need && share_elements(x, m, k, ldx, y, m, n, ldy, type_bytes(type))) return EMB_EINVAL;
   return status(launch_linear(x, type, m, k, ldx, w, n, y, ldy, workspace, S(stream)));
 }
 

@@ -141,7 +141,8 @@ def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
 
 
 def linear(x, w: Mx4Matrix, out=None):
-    """Q(x) w^T for full-precision rows x [m, k] and a weight w [n, k] in 4 bits, in the type of x."""
+    """Q(x) w^T for full-precision rows x [m, k] and a weight w [n, k] in 4 bits, in the type of x.  An `out` over x is
+    refused where the rows are quantised inside the product (few of them)."""
     p, t, m, k, ld = lib.matrix(x, "x")
     dev = x.device
     if k != w.cols or w.device != dev:

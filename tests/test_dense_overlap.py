@@ -1,0 +1,43 @@
+"""An output over its own input: the linear layer's route that quantises its rows inside the product refuses it (its
+workgroups read all of x while others write y).  No GPU: a call that passes the checks ends at the launch."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2010_11305_amd import dense_lib
+from paper_2010_11305_amd import emb_cache as ec
+
+FAKE = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def L():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the calls use addresses that no GPU may touch")
+    if not os.path.exists(ec.LIB_PATH):
+        from paper_2010_11305_amd import build
+        build.build()
+    return dense_lib.load()
+
+
+@pytest.mark.parametrize("y,ldx,ldy,shared", [
+    (0, 64, 64, True), (-1, 64, 64, True), (3 * 64 + 63, 64, 64, True), (3 * 64 + 64, 64, 64, False), (-4 * 64, 64, 64, False),
+    (-3 * 64 - 1, 64, 64, True), (64, 128, 128, False), (63, 128, 128, True), (-64, 128, 128, False), (-63, 128, 128, True),
+    (128 + 64, 128, 128, False), (-128 - 64, 128, 128, False), (2 * 128 + 65, 128, 128, True), (64, 128, 129, True),
+])
+def test_rows_quantised_inside(L, y, ldx, ldy, shared):
+    """x [4][64] and y [4][64], `y` elements behind x."""
+    n = ctypes.c_size_t(1)
+    assert L.emb_mx4_linear_workspace(4, 64, 64, ctypes.byref(n)) == 0 and n.value == 0
+    for type, b in ((0, 4), (1, 2)):
+        st = L.emb_mx4_linear(FAKE, type, 4, 64, ldx, 2 * FAKE, 64, FAKE + y * b, ldy, None, 0, None)
+        assert (st == ec.EMB_EINVAL) == shared
+
+
+def test_rows_quantised_before(L):
+    """With a workspace the rows are read before anything is written."""
+    n = ctypes.c_size_t()
+    assert L.emb_mx4_linear_workspace(200, 64, 64, ctypes.byref(n)) == 0 and n.value
+    assert L.emb_mx4_linear(FAKE, 1, 200, 64, 64, 2 * FAKE, 64, FAKE, 64, 3 * FAKE, n.value, None) != ec.EMB_EINVAL
