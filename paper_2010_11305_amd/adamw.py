@@ -96,10 +96,10 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
         # a model has hundreds of tensors and a step lasts some hundred microseconds: C-level maps, one a property
-        given, sizes = grads, self.sizes
-        if any(g is None for g in grads):
+        given, sizes, changed = grads, self.sizes, self.params
+        if type(None) in set(map(type, grads)):
             kept = [k for k, g in enumerate(grads) if g is not None]
-            given, sizes = [grads[k] for k in kept], [sizes[k] for k in kept]
+            given, sizes, changed = ([of[k] for k in kept] for of in (grads, sizes, changed))
         index = self.device.index
         if (list(map(Tensor.numel, given)) != sizes or not all(map(Tensor.is_contiguous, given))
                 or not set(map(dtype_of, given)) <= {self.grad_dtype} or not set(map(Tensor.get_device, given)) <= {index}):
@@ -115,6 +115,7 @@ class AdamW:
         gp = array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
         lib.call("emb_adamw_step", self.device, self._h, pp.buffer_info()[0], gp.buffer_info()[0],
                  self.lr if lr is None else float(lr), scale)
+        lib.written(changed)
 
     def state(self) -> dict:
         """The moments, as views of the state buffer over all tensors, each tensor's part padded to a multiple of 32

@@ -5,6 +5,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import emb_cache
 
@@ -97,6 +98,15 @@ def call(name: str, device, *args):
             status = f(*args, torch._C._cuda_getCurrentRawStream(index))
     if status:
         raise emb_cache.EmbCacheError(status, name)
+
+
+def written(tensors):
+    """Count tensors that a kernel wrote in place as changed: a backward pass that had kept one raises then, as it
+    does for torch's own operations in place."""
+    try:
+        increment_version(tensors)
+    except RuntimeError:    # some are of inference mode and have no such count
+        increment_version([t for t in tensors if not t.is_inference()])
 
 
 def rounding_of(name: str) -> int:

@@ -2,7 +2,8 @@
 
 A block of 32 consecutive values of a row shares a power of two; each value is a 4-bit code
 (sign, 2 exponent bits, 1 mantissa bit).  The bindings only marshal arguments; every step
-runs in the HIP kernels of libembcache, on the current stream.
+runs in the HIP kernels of libembcache, on the current stream.  None of it is recorded by autograd: what
+comes out has no history, whatever went in (Linear.backward gives the gradients).
 
     w4 = mx4.quantize(w)                   # [n, k]
     y = mx4.linear(x, w4)                  # [m, n] = Q(x) w4^T, x in full precision
@@ -61,8 +62,11 @@ class Mx4Matrix:
     def dequantize(self, dtype=torch.float32, out=None):
         """The values as a [rows, cols] tensor (exact in float32 and bfloat16)."""
         rows, cols, dev = self.rows, self.cols, self.data.device
+        given = out is not None
         out, p, t, ld = _result(out, rows, cols, dtype, dev)
         lib.call("emb_mx4_dequantize", dev, self.data.data_ptr(), rows, cols, p, t, ld)
+        if given:
+            lib.written([out])
         return out
 
     def to_codes(self):
@@ -134,9 +138,11 @@ def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
     """a b^T for a [m, k] and b [n, k]: FP32 sums, one rounding to dtype (or to out's)."""
     if a.cols != b.cols or a.device != b.device:
         raise ValueError(f"a {a.shape} and b {b.shape} must have the same number of columns, on one device")
-    dev = a.device
+    dev, given = a.device, out is not None
     out, p, t, ld = _result(out, a.rows, b.rows, dtype, dev)
     lib.call("emb_mx4_matmul", dev, a.data.data_ptr(), b.data.data_ptr(), a.rows, b.rows, a.cols, p, t, ld)
+    if given:
+        lib.written([out])
     return out
 
 
@@ -144,7 +150,7 @@ def linear(x, w: Mx4Matrix, out=None):
     """Q(x) w^T for full-precision rows x [m, k] and a weight w [n, k] in 4 bits, in the type of x.  An `out` over x is
     refused where the rows are quantised inside the product (few of them)."""
     p, t, m, k, ld = lib.matrix(x, "x")
-    dev = x.device
+    dev, given = x.device, out is not None
     if k != w.cols or w.device != dev:
         raise ValueError(f"x [{m}, {k}] and w {w.shape} must have the same number of columns, on one device")
     out, yp, yt, yld = _result(out, m, w.rows, x.dtype, dev)
@@ -153,6 +159,8 @@ def linear(x, w: Mx4Matrix, out=None):
     need = _query("emb_mx4_linear_workspace", m, w.rows, k)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     lib.call("emb_mx4_linear", dev, p, t, m, k, ld, w.data.data_ptr(), w.rows, yp, yld, ws.data_ptr() if need else None, need)
+    if given:
+        lib.written([out])
     return out
 
 
