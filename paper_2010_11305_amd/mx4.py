@@ -85,6 +85,8 @@ def from_codes(codes, scales, cols: int, out: Mx4Matrix | None = None) -> Mx4Mat
     for t, width, what in ((codes, -(-cols // 2), "codes"), (scales, -(-cols // 32), "scales")):
         if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != (rows, width):
             raise ValueError(f"{what} must be a contiguous uint8 tensor [{rows}, {width}] on the GPU")
+    if codes.device != scales.device:
+        raise ValueError(f"codes and scales must be on one device, not {codes.device} and {scales.device}")
     out = _target(out, rows, cols, codes.device, "out")
     lib.call("emb_mx4_pack", out.device, codes.data_ptr(), scales.data_ptr(), rows, cols, out.data.data_ptr())
     return out
