@@ -58,8 +58,8 @@ int emb_mx4_query_bytes(int64_t rows, int64_t cols, size_t* bytes);
 
 /* Quantise x [rows][cols] (row stride ld >= cols, in elements; any alignment of
  * the type) into by_rows, an MX4 matrix [rows][cols], and into by_columns, the MX4
- * matrix [cols][rows] of its transpose.  Either may be NULL; with both, x is read
- * once.  rounding: EMB_ROUND_NEAREST or EMB_ROUND_STOCHASTIC (seed and step are
+ * matrix [cols][rows] of its transpose.  Either may be NULL; with both, which must not overlap, x is
+ * read once.  rounding: EMB_ROUND_NEAREST or EMB_ROUND_STOCHASTIC (seed and step are
  * used by the latter).  Enqueue-only. */
 int emb_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, void* by_rows,
                      void* by_columns, int32_t rounding, uint64_t seed, uint32_t step, void* stream);

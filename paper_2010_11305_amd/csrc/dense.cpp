@@ -115,6 +115,9 @@ int quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld
   if (rows == 0 || cols == 0) return EMB_OK;
   if (!matrix_ok(x, type, rows, cols, ld) || (!by_rows && !by_columns)) return EMB_EINVAL;
   if (!aligned(by_rows) || !aligned(by_columns)) return EMB_EINVAL;
+  const uintptr_t r = reinterpret_cast<uintptr_t>(by_rows), c = reinterpret_cast<uintptr_t>(by_columns);
+  if (r && c && r < c + (uintptr_t)Mx4(nullptr, cols, rows).bytes() && c < r + (uintptr_t)Mx4(nullptr, rows, cols).bytes())
+    return EMB_EINVAL;   // one kernel writes both
   return status(launch_quantize(x, type, rows, cols, ld, by_rows, by_columns, rounding, seed, step, draws, S(stream)));
 }
 

@@ -1,5 +1,6 @@
-"""An output over its own input: the linear layer's route that quantises its rows inside the product refuses it (its
-workgroups read all of x while others write y).  No GPU: a call that passes the checks ends at the launch."""
+"""Buffers of a call that overlap.  The two results of a quantisation are refused.  An output over its own input: the
+linear layer's route that quantises its rows inside the product refuses it (its workgroups read all of x while
+others write y).  No GPU: a call that passes the checks ends at the launch."""
 import ctypes
 import os
 
@@ -41,3 +42,16 @@ def test_rows_quantised_before(L):
     n = ctypes.c_size_t()
     assert L.emb_mx4_linear_workspace(200, 64, 64, ctypes.byref(n)) == 0 and n.value
     assert L.emb_mx4_linear(FAKE, 1, 200, 64, 64, 2 * FAKE, 64, FAKE, 64, 3 * FAKE, n.value, None) != ec.EMB_EINVAL
+
+
+@pytest.mark.parametrize("columns,shared", [(0, True), (256, True), (-256, True), (4 * 1280, False), (-4 * 1280, False),
+                                            (4 * 1280 - 256, True)])
+def test_both_results_of_a_quantisation(L, columns, shared):
+    """[64][64]: 4 tiles and 4 pieces of scale bytes either way."""
+    n = ctypes.c_size_t()
+    assert L.emb_mx4_query_bytes(64, 64, ctypes.byref(n)) == 0 and n.value == 4 * 1280
+    st = L.emb_mx4_quantize(FAKE, 0, 64, 64, 64, 4 * FAKE, 4 * FAKE + columns, 0, 0, 0, None)
+    assert (st == ec.EMB_EINVAL) == shared
+    m = L.emb_mx4_linear_train(FAKE, 0, 64, 64, 64, 2 * FAKE, 16, 3 * FAKE, 16, 4 * FAKE + columns, 0, 0, 0, 4 * FAKE, 4 * 1280,
+                               None)
+    assert (m == ec.EMB_EINVAL) == shared
