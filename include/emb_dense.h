@@ -194,7 +194,7 @@ int emb_adamw_destroy(emb_adamw_t h);
 int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads, double lr, const float* grad_scale,
                    void* stream);
 
-/* Steps done (t of the next step minus 1). */
+/* Steps done (t of the next step minus 1), 0 .. 2^63 - 1. */
 int emb_adamw_get_step(emb_adamw_t h, uint64_t* step);
 int emb_adamw_set_step(emb_adamw_t h, uint64_t step);
 

@@ -18,6 +18,9 @@ hipStream_t S(void* s) { return reinterpret_cast<hipStream_t>(s); }
 int status(hipError_t e) { return e == hipSuccess ? EMB_OK : EMB_EHIP; }
 bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % kAlign == 0; }
 
+// Steps that a counter may be set to: the next one is above 0, and a negative number of a binding is none.
+constexpr uint64_t kMaxStep = (uint64_t)INT64_MAX;
+
 int type_bytes(int32_t type) { return type == EMB_TYPE_FP32 ? 4 : 2; }
 bool type_ok(int32_t type) { return type == EMB_TYPE_FP32 || type == EMB_TYPE_BF16 || type == EMB_TYPE_FP16; }
 bool rounding_ok(int32_t r) { return r == EMB_ROUND_NEAREST || r == EMB_ROUND_STOCHASTIC; }
@@ -343,7 +346,7 @@ int emb_adamw_get_step(emb_adamw_t h, uint64_t* step) {
 }
 
 int emb_adamw_set_step(emb_adamw_t h, uint64_t step) {
-  if (!h) return EMB_EINVAL;
+  if (!h || step > kMaxStep) return EMB_EINVAL;
   h->step = step;
   return EMB_OK;
 }

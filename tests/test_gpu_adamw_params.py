@@ -79,3 +79,18 @@ def test_shared_memory_is_refused(torch):
     with pytest.raises(ValueError):
         opt.step([torch.ones(n, device="cuda") for n in (50, 50, 10, 0)])
     assert (base == 0).all()
+
+
+def test_steps_that_a_counter_may_hold(torch):
+    """A negative number wraps round to a huge one, and 2^64 - 1 is followed by step 0, whose corrections divide by 0."""
+    from paper_2010_11305_amd.emb_cache import EmbCacheError
+
+    params, opt = make(torch)
+    for bad in (-1, -5, 2**63):
+        with pytest.raises(EmbCacheError):
+            opt.step_count = bad
+        assert opt.step_count == 0
+    for good in (2**63 - 1, 10**12, 1000):
+        opt.step_count = good
+        opt.step(grads_of(torch, params))
+        assert opt.step_count == good + 1 and all(torch.isfinite(p).all() for p in params)
