@@ -187,7 +187,7 @@ int emb_adamw_destroy(emb_adamw_t h);
 
 /* One step.  params and grads: host arrays of num_tensors device pointers (read during
  * the call only), each tensor contiguous, at any alignment of its type, no parameter in the memory of
- * another.  A tensor whose gradient is NULL keeps its parameters and moments.  grad_scale: a device FP32 factor of
+ * another.  A tensor whose gradient is NULL keeps its parameters and moments.  grad_scale: an aligned device FP32 factor of
  * every gradient (what a clipped norm leaves, say), or NULL for 1.  The step counter
  * increases by one; it lives on the host, so a call captured into a HIP graph repeats the
  * constants and draws of the step it was captured in.  Enqueue-only. */

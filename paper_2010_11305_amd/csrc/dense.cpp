@@ -299,7 +299,7 @@ int emb_adamw_destroy(emb_adamw_t h) {
 
 int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads, double lr, const float* grad_scale,
                    void* stream) {
-  if (!h || !params || !grads || !std::isfinite(lr)) return EMB_EINVAL;
+  if (!h || !params || !grads || !std::isfinite(lr) || reinterpret_cast<uintptr_t>(grad_scale) % 4) return EMB_EINVAL;
   const int T = (int)h->sizes.size();
   const size_t pb = type_bytes(h->param_type), gb = type_bytes(h->grad_type);
   for (int t = 0; t < T; ++t) {

@@ -94,3 +94,18 @@ def test_steps_that_a_counter_may_hold(torch):
         opt.step_count = good
         opt.step(grads_of(torch, params))
         assert opt.step_count == good + 1 and all(torch.isfinite(p).all() for p in params)
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_a_factor_at_an_odd_address_is_refused(torch, off):
+    from array import array
+
+    from paper_2010_11305_amd import dense_lib
+    from paper_2010_11305_amd.emb_cache import EmbCacheError
+
+    params, opt = make(torch)
+    scale, grads = torch.ones(2, device="cuda"), grads_of(torch, params)
+    p, g = (array("Q", [t.data_ptr() for t in ts]) for ts in (params, grads))
+    with pytest.raises(EmbCacheError):
+        dense_lib.call("emb_adamw_step", opt.device, opt._h, p.buffer_info()[0], g.buffer_info()[0], 1e-3, scale.data_ptr() + off)
+    assert opt.step_count == 0
