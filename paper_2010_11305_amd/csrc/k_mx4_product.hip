@@ -110,7 +110,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t lane_offset, 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
                : "s"(lds), "v"(lane_offset), "s"(srd), "s"(offset)
-               : "memory");
+               : "memory", "m0");
 }
 
 // All but the last IN_FLIGHT of the wave's loads to LDS have arrived, and its reads of LDS are
