@@ -65,7 +65,9 @@ int emb_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, in
                      void* by_columns, int32_t rounding, uint64_t seed, uint32_t step, void* stream);
 
 /* The values that q [rows][cols] stands for, in x [rows][cols] with row stride ld.
- * Exact in FP32 and BF16; FP16 rounds to nearest even.  Enqueue-only. */
+ * Exact in FP32 and BF16, FP16 rounds to nearest even; infinite beyond the type's largest value, which in
+ * FP32 and BF16 only scale bytes 253 and 254 reach (packed ones: quantisation ends at 252).
+ * Enqueue-only. */
 int emb_mx4_dequantize(const void* q, int64_t rows, int64_t cols, void* x, int32_t type, int64_t ld, void* stream);
 
 /* Between an MX4 matrix and plain codes: codes [rows][ceil(cols / 2)], two a byte, the

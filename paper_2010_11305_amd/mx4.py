@@ -60,7 +60,8 @@ class Mx4Matrix:
         return self.data.device
 
     def dequantize(self, dtype=torch.float32, out=None):
-        """The values as a [rows, cols] tensor (exact in float32 and bfloat16)."""
+        """The values as a [rows, cols] tensor, exact in float32 and bfloat16 (beyond 2^128, which only imported scale
+        bytes 253 and 254 reach, infinite)."""
         rows, cols, dev = self.rows, self.cols, self.data.device
         given = out is not None
         out, p, t, ld = _result(out, rows, cols, dtype, dev)
@@ -195,6 +196,7 @@ class Linear:
         quantize_both(weight, self.rounding, self.weight_seed, step, (self.by_rows, self.by_columns))
 
     def forward(self, x):
+        """y for serving: the rows round to nearest whatever `rounding` says, so that an answer is no draw."""
         return linear(x, self.by_rows)
 
     def forward_train(self, x, step=0):

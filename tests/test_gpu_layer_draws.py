@@ -82,3 +82,17 @@ def test_streams_of_the_operands(torch, m, n, k):
     for got, a, b in ((y, q(X, 2, SEED, 8), q(W, 0, own, 7)), (dx, q(D, 0, SEED, 9), q(W.T, 1, own, 7)),
                       (dw, q(D.T, 1, SEED, 9), q(X.T, 3, SEED, 8))):
         assert (np.abs(plain(got) - a @ b.T) <= a.shape[1] * 2.0**-23 * (np.abs(a) @ np.abs(b).T) + 2.0**-24 * np.abs(a @ b.T)).all()
+
+
+def test_serving_draws_nothing(torch):
+    """forward() rounds its rows to nearest, also where training rounds them stochastically."""
+    from paper_2010_11305_amd import mx4
+
+    x, w = (torch.from_numpy(spread(40, 96, i)).bfloat16().cuda() for i in (1, 2))
+    layer = mx4.Linear(40, 96, rounding="stochastic", seed=SEED)
+    layer.load(w, step=3)
+    want = ref.mx4_round_trip(plain(x)) @ plain(layer.by_rows.dequantize()).T
+    for _ in range(2):
+        y = plain(layer.forward(x))
+        assert (np.abs(y - want) <= (96 * 2.0**-23 + 2.0**-8) * want).all()
+    assert torch.equal(layer.forward(x), mx4.linear(x, layer.by_rows))
