@@ -104,7 +104,7 @@ int emb_mx4_linear(const void* x, int32_t type, int64_t m, int64_t k, int64_t ld
  *   dx [m][k] = Q(dy) Q(w^T)^T   in the type of dy, w_columns the MX4 matrix [k][n] of w^T
  *   dw [n][k] = Q(dy^T) saved^T  in dw_type
  * The rounding of the codes is the gradients' only approximation: as usual they are those
- * of the unrounded layer, taken at the rounded values.
+ * of the unrounded layer, taken at the rounded values.  The depths of its products are n and m: both at most 2^24.
  *
  * workspace: the bytes that the function's own query reports, 256-byte aligned, or NULL when
  * that is 0.  Enqueue-only. */
@@ -189,8 +189,8 @@ int emb_adamw_destroy(emb_adamw_t h);
 
 /* One step.  params and grads: host arrays of num_tensors device pointers (read during
  * the call only), each tensor contiguous, at any alignment of its type, no parameter in the memory of
- * another.  A tensor whose gradient is NULL keeps its parameters and moments.  grad_scale: an aligned device FP32 factor of
- * every gradient (what a clipped norm leaves, say), or NULL for 1.  The step counter
+ * another.  A tensor whose gradient is NULL keeps its parameters and moments.  grad_scale: an
+ * aligned device FP32 factor of every gradient (what a clipped norm leaves, say), or NULL for 1.  The step counter
  * increases by one; it lives on the host, so a call captured into a HIP graph repeats the
  * constants and draws of the step it was captured in.  Enqueue-only. */
 int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads, double lr, const float* grad_scale,

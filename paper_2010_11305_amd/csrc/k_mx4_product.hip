@@ -3,9 +3,12 @@
 // an MX4 matrix holds lane by lane.  Codes and scales go from memory to the instruction as they lie.
 //
 // k_product: tiles of C of 256, 128 or 64 rows and columns, the operands staged in LDS.  16384 x 8192 x 12800: 642 to
-// 770 us from card to card, 5.4 to 4.5 PFLOP/s.  The bound is power: on normal values the clock falls from 2.4 to
-// 1.6 GHz (560 us and 2.4 GHz on zeros, where a step takes 1190 cycles of the 1024 that its instructions issue for).
-// The 32x32x64 instruction needs 6% fewer cycles and takes 2% longer.
+// 780 us from card to card, 5.4 to 4.4 PFLOP/s.  Two things bound it.  Power: on normal values the clock is 1.6 GHz, on
+// zeros 2.2 (575 us), with the same 1.25 to 1.27M cycles.  And the cycles, of which the matrix pipes are busy for 65%:
+// a step of 128 columns takes 1375 to 1415 (by the time's slope over K, whatever the values) and its instructions
+// issue for 1024; start and end of a 256 x 256 tile take some 18000 more.  Of a wave's time 59% issues, 23% waits for
+// its turn to issue and 18% at waits and barriers; LDS reads are active for 20% and stall nothing (0.1%).  The 32x32x64
+// instruction needs 6% fewer cycles and takes 2% longer.
 // k_skinny: few rows against a weight that is read once.  1 row, 4096 x 12800: 5.3 us for 27.9 MB, much of it
 // from the last-level cache; 1 row, 32000 x 4096: 14.9 us, 4.7 TB/s.
 #include <type_traits>
