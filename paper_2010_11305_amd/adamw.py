@@ -17,6 +17,7 @@ from torch import Tensor
 from . import dense_lib as lib
 
 dtype_of = attrgetter("dtype")
+NOWHERE = 2**64 - 1    # the address of no tensor
 
 
 class AdamW:
@@ -61,20 +62,25 @@ class AdamW:
                                          torch.cuda.current_stream().cuda_stream, ctypes.byref(self._h)),
                       "emb_adamw_create")
 
-    def _hold(self):
-        """Check the parameters and keep their memory by views of it: as long as a parameter's address is that of its
-        view, nothing else can have come to lie there, and step() need not look at type, device and size again."""
-        for p, size in zip(self.params, self.sizes):
+    def _hold(self, which=None):
+        """Check the parameters (those of `which` alone: a step writes no other) and keep their memory by views of it: as
+        long as a parameter's address is that of its view, nothing else can have come to lie there, and step() need not
+        look at type, device and size again."""
+        which = range(len(self.params)) if which is None else which
+        places = []
+        for p, size in ((self.params[k], self.sizes[k]) for k in which):
             if (p.dtype != self.dtype or p.device != self.device or not p.is_cuda or not p.is_contiguous()
                     or p.numel() != size):
                 raise ValueError("params must be contiguous tensors of one type on one GPU, and keep type, device and size")
+            if size:
+                places.append((p.data_ptr(), size * p.element_size()))
         end = 0
-        for start, size in sorted((p.data_ptr(), p.numel() * p.element_size()) for p in self.params if p.numel()):
+        for start, size in sorted(places):
             if start < end:
                 raise ValueError("params must not share memory (a tied parameter is given once)")
             end = start + size
-        self._held = [p.detach() for p in self.params]
-        self._pointers = array("Q", map(Tensor.data_ptr, self._held))
+        self._held = {k: self.params[k].detach() for k in which}
+        self._pointers = array("Q", [self._held[k].data_ptr() if k in self._held else NOWHERE for k in range(len(self.params))])
         # a tensor of one dimension and the same elements cannot lie otherwise
         self._wide = [p for p in self.params if p.dim() > 1]
 
@@ -96,7 +102,7 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
         # a model has hundreds of tensors and a step lasts some hundred microseconds: C-level maps, one a property
-        given, sizes, changed = grads, self.sizes, self.params
+        given, sizes, changed, kept = grads, self.sizes, self.params, None
         if type(None) in set(map(type, grads)):
             kept = [k for k, g in enumerate(grads) if g is not None]
             given, sizes, changed = ([of[k] for k in kept] for of in (grads, sizes, changed))
@@ -111,7 +117,7 @@ class AdamW:
             scale = grad_scale.data_ptr()
         pp = array("Q", map(Tensor.data_ptr, self.params))
         if pp != self._pointers or not all(map(Tensor.is_contiguous, self._wide)):
-            self._hold()   # another storage, as a parameter's `data` may be given
+            self._hold(kept)   # another storage, as a parameter's `data` may be given
         gp = array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
         lib.call("emb_adamw_step", self.device, self._h, pp.buffer_info()[0], gp.buffer_info()[0],
                  self.lr if lr is None else float(lr), scale)

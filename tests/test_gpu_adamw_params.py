@@ -109,3 +109,25 @@ def test_a_factor_at_an_odd_address_is_refused(torch, off):
     with pytest.raises(EmbCacheError):
         dense_lib.call("emb_adamw_step", opt.device, opt._h, p.buffer_info()[0], g.buffer_info()[0], 1e-3, scale.data_ptr() + off)
     assert opt.step_count == 0
+
+
+@pytest.mark.parametrize("elsewhere", ["cpu", "empty", "type"])
+def test_a_parameter_without_a_gradient_may_be_elsewhere(torch, elsewhere):
+    """Nothing of it is read or written; once it has a gradient it must be what it was."""
+    params, opt = make(torch)
+    other, same = make(torch)
+    for p, q in zip(params, other):
+        q.data.copy_(p.data)
+    home = params[1].data
+    params[1].data = {"cpu": home.cpu, "empty": lambda: home[:0, :0], "type": home.half}[elsewhere]()
+    grads = grads_of(torch, other)
+    for _ in range(2):
+        opt.step([grads[0], None, grads[2]])
+        same.step([grads[0], None, grads[2]])
+    with pytest.raises(ValueError):
+        opt.step(grads)
+    params[1].data = home
+    opt.step(grads)
+    same.step(grads)
+    assert opt.step_count == same.step_count == 3
+    assert all(torch.equal(p, q) for p, q in zip(params, other))
