@@ -41,18 +41,19 @@ bool matrix_ok(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t 
   return (double)rows * (double)ld * type_bytes(type) <= 4.0 * kMaxBytes;
 }
 
-// Whether two matrices share an element: by their extents, or, where their rows lie equally far apart, by the
-// columns that each takes of them.
+// Whether two matrices (of few rows) share an element.
 bool share_elements(const void* x, int64_t x_rows, int64_t x_cols, int64_t x_ld, const void* y, int64_t y_rows, int64_t y_cols,
                     int64_t y_ld, int64_t bytes) {
   if (!x_rows || !x_cols || !y_rows || !y_cols) return false;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
-  const uintptr_t a_end = a + (uintptr_t)(((x_rows - 1) * x_ld + x_cols) * bytes);
-  const uintptr_t b_end = b + (uintptr_t)(((y_rows - 1) * y_ld + y_cols) * bytes);
-  if (a_end <= b || b_end <= a) return false;
-  if (x_ld != y_ld) return true;
-  const uintptr_t row = (uintptr_t)(x_ld * bytes), behind = b >= a ? (b - a) % row : (row - (a - b) % row) % row;
-  return behind < (uintptr_t)(x_cols * bytes) || behind + (uintptr_t)(y_cols * bytes) > row;
+  const int64_t to = (int64_t)(reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(x));
+  const int64_t xw = x_cols * bytes, xs = x_ld * bytes, yw = y_cols * bytes, ys = y_ld * bytes;
+  if (to >= (x_rows - 1) * xs + xw || to + (y_rows - 1) * ys + yw <= 0) return false;
+  for (int64_t i = 0; i < x_rows; ++i) {
+    const int64_t before = i * xs - to - yw;                 // rows of y that start there or earlier end before row i of x
+    const int64_t k = before < 0 ? 0 : before / ys + 1;
+    if (k < y_rows && to + k * ys < i * xs + xw) return true;
+  }
+  return false;
 }
 
 }  // namespace

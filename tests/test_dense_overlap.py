@@ -27,6 +27,9 @@ def L():
     (0, 64, 64, True), (-1, 64, 64, True), (3 * 64 + 63, 64, 64, True), (3 * 64 + 64, 64, 64, False), (-4 * 64, 64, 64, False),
     (-3 * 64 - 1, 64, 64, True), (64, 128, 128, False), (63, 128, 128, True), (-64, 128, 128, False), (-63, 128, 128, True),
     (128 + 64, 128, 128, False), (-128 - 64, 128, 128, False), (2 * 128 + 65, 128, 128, True), (64, 128, 129, True),
+    # rows that lie differently far apart: between each other, or not
+    (70, 140, 139, False), (-70, 139, 140, False), (70, 140, 150, True), (-3 * 140 + 70, 139, 140, False), (-3 * 140 + 75, 139, 140, False),
+    (-3 * 140 + 76, 139, 140, True),
 ])
 def test_rows_quantised_inside(L, y, ldx, ldy, shared):
     """x [4][64] and y [4][64], `y` elements behind x."""
@@ -55,3 +58,21 @@ def test_both_results_of_a_quantisation(L, columns, shared):
     m = L.emb_mx4_linear_train(FAKE, 0, 64, 64, 64, 2 * FAKE, 16, 3 * FAKE, 16, 4 * FAKE + columns, 0, 0, 0, 4 * FAKE, 4 * 1280,
                                None)
     assert (m == ec.EMB_EINVAL) == shared
+
+
+def test_against_every_element(L):
+    """Drawn strides and places against sets of elements."""
+    import random
+
+    r, seen = random.Random(4), set()
+    for _ in range(400):
+        m, k, n = r.randint(1, 9), r.randint(1, 40), r.randint(1, 40)
+        ldx, ldy = k + r.randint(0, 60), n + r.randint(0, 60)
+        if r.random() < 0.5:
+            ldx = ldy = max(ldx, ldy)
+        y = r.randint(-m * ldy - 5, m * ldx + 5)
+        shared = bool({i * ldx + j for i in range(m) for j in range(k)} & {y + i * ldy + j for i in range(m) for j in range(n)})
+        st = L.emb_mx4_linear(FAKE, 0, m, k, ldx, 2 * FAKE, n, FAKE + 4 * y, ldy, None, 0, None)
+        assert (st == ec.EMB_EINVAL) == shared, (m, k, n, ldx, ldy, y)
+        seen.add((shared, ldx == ldy))
+    assert len(seen) == 4
