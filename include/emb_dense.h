@@ -4,11 +4,16 @@
  * int status codes, caller-owned device memory, `stream` a hipStream_t passed as
  * void*, calls that only enqueue kernels unless they say otherwise.
  *
- * Two groups:
- *   emb_mx4_*    matrices in microscaled 4-bit floating point ("MX4"): quantisation
- *                along either axis, expansion, the product of two of them, and the
- *                linear layer on full-precision rows;
- *   emb_adamw_*  one AdamW step over many tensors, with moments in FP32 or 8 bits.
+ * Five groups:
+ *   emb_mx4_*      matrices in microscaled 4-bit floating point ("MX4"): quantisation
+ *                  along either axis, expansion, the product of two of them, and the
+ *                  linear layer on full-precision rows;
+ *   emb_adamw_*    one AdamW step over many tensors, with moments in FP32 or 8 bits;
+ *   emb_rmsnorm_*  the root-mean-square norm of rows with a residual's addition, its
+ *                  gradients, and its output in 8 bits;
+ *   emb_w4_*       matrices in 4-bit integer codes with a scale and a bias per group, and
+ *                  their product with few rows (in full precision or 8 bits);
+ *   emb_clip_*     the norm of many gradients together, and their scaling.
  *
  * MX4.  A block is 32 consecutive values of a row (the last of a row may be
  * shorter).  With a = max |x| over the block it has one power of two
@@ -199,6 +204,132 @@ int emb_adamw_step(emb_adamw_t h, void* const* params, const void* const* grads,
 /* Steps done (t of the next step minus 1), 0 .. 2^63 - 1. */
 int emb_adamw_get_step(emb_adamw_t h, uint64_t* step);
 int emb_adamw_set_step(emb_adamw_t h, uint64_t step);
+
+/* ---- Root-mean-square norm ------------------------------------------------------------------
+ * Of each row of h = x + residual (rounded to the type of x; x itself without a residual):
+ *   inverse = 1 / sqrt(mean(h^2) + eps),  y = h * inverse * gain
+ * The sum of squares is taken in FP64 (no FP32 value overflows it), inverse is rounded to FP32, both products
+ * are FP32 operations, and y is rounded once to the type of x (nearest even).
+ *
+ * x, residual, sum and y: [rows][cols] in `type`, each with its own row stride, at any alignment of the type.
+ *   residual    NULL for none
+ *   sum         h, or NULL where it is not wanted (without a residual it must be NULL)
+ *   gain        [cols] in gain_type (EMB_TYPE_FP32, or `type`), NULL for ones
+ *   eps         a positive normal number
+ *   inverse     [rows] FP32 for the backward pass, or NULL
+ * sum and y may each be x or the residual itself (same address and stride); no other elements may be shared.
+ * rows may be 0, cols not.  Enqueue-only. */
+int emb_rmsnorm_forward(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, const void* residual,
+                        int64_t ldr, const void* gain, int32_t gain_type, float eps, void* sum, int64_t lds, void* y,
+                        int64_t ldy, float* inverse, void* stream);
+
+/* The same with its rows in 8 bits: with v = h * inverse * gain in FP32 and a = max |v| of the row,
+ *   scale = max(a / 127, 2^-126),  code = v * (1 / scale) rounded to nearest even, -127 .. 127.
+ * codes [rows][ldc] (no alignment), scales [rows].  A row with a value v that is not finite has codes 0 and the
+ * scale NaN: it stands for NaN.  Enqueue-only. */
+int emb_rmsnorm_forward8(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, const void* residual,
+                         int64_t ldr, const void* gain, int32_t gain_type, float eps, void* sum, int64_t lds,
+                         int8_t* codes, int64_t ldc, float* scales, void* stream);
+
+/* code * scale, rounded to `type`.  Enqueue-only. */
+int emb_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,
+                         int32_t type, int64_t ldx, void* stream);
+
+/* Gradients for dy [rows][cols], the gradient of y, with n = h * inverse and dn = dy * gain:
+ *   dx = (dn - n * mean(dn * n)) * inverse + dsum   in `type`: the gradient of x and of the residual alike
+ *   dgain = sum over the rows of dy * n             in gain_type
+ * h and inverse are those of the forward pass; dsum [rows][cols] is what reaches h past the norm, or NULL.  dgain NULL
+ * where it is not wanted.  Sums in FP32 over at most 256 rows, those joined in FP64, in an order that is a
+ * function of the sizes.  dx may be dy, h or dsum itself; no other elements may be shared.
+ * workspace: emb_rmsnorm_backward_workspace bytes, 256-byte aligned, or NULL when that is 0.  Enqueue-only. */
+int emb_rmsnorm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes);
+int emb_rmsnorm_backward(const void* dy, int32_t type, int64_t rows, int64_t cols, int64_t lddy, const void* h, int64_t ldh,
+                         const float* inverse, const void* gain, int32_t gain_type, const void* dsum, int64_t ldds,
+                         void* dx, int64_t lddx, void* dgain, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- 4-bit weights with group scales --------------------------------------------------------
+ * "W4": each `group` (32, 64 or 128) consecutive columns of a row, the last of a row maybe fewer, have a scale and a
+ * bias in FP16 and codes q of 0 .. 15, and stand for bias + scale * q: the form of the tables' INT4 rows, by groups.
+ * Quantisation, over a group's values:
+ *   scale = (max - min) / 15, bias = min, both rounded to FP16 (nearest even);
+ *   q = (w - bias) / scale rounded to nearest even, within 0 .. 15; 0 where scale is 0.
+ * A group with a value that is not finite, or of 65520 and more, which FP16 does not hold, has scale and bias NaN.
+ *
+ * A W4 matrix [rows][cols] is one device buffer of emb_w4_query_bytes, 256-byte aligned: tiles of 16 rows x 128 columns,
+ * 1024 bytes each, row tiles outermost; in a tile the 16 bytes at 16 (16 b + r) hold columns 32 i + 8 b + j (j = 0 .. 7)
+ * of row r in dword i (0 .. 3), column j < 4 in nibble 2 j and j >= 4 in nibble 2 (j - 4) + 1.  Then, for each row tile
+ * and each of its groups, 16 pairs (scale, bias).  Codes, scales and biases past the last row or column are 0. */
+#define EMB_TYPE_INT8 3 /* rows in 8 bits with a scale each (emb_w4_linear alone) */
+
+/* Bytes of a W4 matrix (0 when it has no element).  rows, cols: 0 .. 2^31 - 1.  Host only. */
+int emb_w4_query_bytes(int64_t rows, int64_t cols, int32_t group, size_t* bytes);
+int emb_w4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, int32_t group, void* q,
+                    void* stream);
+/* bias + scale * q in FP32, rounded to `type`. */
+int emb_w4_dequantize(const void* q, int64_t rows, int64_t cols, int32_t group, void* x, int32_t type, int64_t ld,
+                      void* stream);
+/* Between a W4 matrix and the plain form: codes [rows][ceil(cols / 2)], two a byte, the even column in the low half;
+ * scales and biases FP16 [rows][ceil(cols / group)]; on the device and without padding.  With an odd number of
+ * columns the last half byte of a row is ignored by pack and 0 from unpack.  Enqueue-only, as the two above. */
+int emb_w4_pack(const uint8_t* codes, const void* scales, const void* biases, int64_t rows, int64_t cols, int32_t group,
+                void* q, void* stream);
+int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint8_t* codes, void* scales, void* biases,
+                  void* stream);
+
+/* y [m][n] = x w^T + bias for rows x [m][k] and a W4 weight w [n][k], then max(y, 0) if `relu` (NaN stays NaN).  Made
+ * for few rows (a weight is read once for each 64 of them); right for any number.
+ *   type      of x: a full-precision type, or EMB_TYPE_INT8 with `scales` [m], the rows' scales (NULL otherwise)
+ *   bias      [n] FP32, or NULL
+ *   y_type    a full-precision type
+ * A group's products are summed over its codes and its biases apart, scale * sum(q x) + bias * sum(x): exact products,
+ * sums in FP32 (of 8-bit rows exact integers within a group), one rounding to y_type.  A row of x that is not finite, or
+ * whose sums with codes of up to 15 overflow FP32, gives values that are not finite.  The order of the sums is a function of type, m, n, k
+ * and group.  y must share no element with x.
+ * workspace: emb_w4_linear_workspace bytes, 256-byte aligned, or NULL when that is 0.  Enqueue-only. */
+int emb_w4_linear_workspace(int32_t type, int64_t m, int64_t n, int64_t k, int32_t group, size_t* bytes);
+int emb_w4_linear(const void* x, int32_t type, const float* scales, int64_t m, int64_t k, int64_t ldx, const void* w,
+                  int64_t n, int32_t group, const float* bias, int32_t relu, void* y, int32_t y_type, int64_t ldy,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The norm of many gradients --------------------------------------------------------------
+ * Over tensors that a model's gradients are:
+ *   norm = sqrt(sum of all squares), factor = min(1, max_norm / norm)
+ * Squares and sums in FP64, in an order that is a function of the sizes alone; both results rounded to FP32.  A NaN
+ * among the gradients makes both NaN; an infinity makes norm infinite and factor 0.  `factor` is what emb_adamw_step
+ * takes as grad_scale; emb_clip_scale multiplies the gradients themselves.
+ *   sizes[t]    elements of tensor t, >= 0
+ *   types[t]    their types, or NULL: `type` for all */
+typedef struct emb_clip_config {
+  int32_t num_tensors;
+  int32_t type;
+  const int64_t* sizes;
+  const int32_t* types;
+} emb_clip_config;
+
+/* state_bytes: the tables that a handle keeps on the device; workspace_bytes: what a call of emb_clip_norm needs. */
+typedef struct emb_clip_sizes {
+  size_t state_bytes;
+  size_t workspace_bytes;
+} emb_clip_sizes;
+
+typedef struct emb_clip* emb_clip_t;
+
+/* Validate `cfg` and report sizes.  Host only. */
+int emb_clip_query_sizes(const emb_clip_config* cfg, emb_clip_sizes* out);
+/* Create a handle over a caller-owned device buffer (256-byte aligned) that must stay allocated until
+ * emb_clip_destroy.  Nothing writes it after this call, so calls with one handle may run at once (each with its
+ * own workspace).  Synchronizes `stream`. */
+int emb_clip_create(const emb_clip_config* cfg, void* state, size_t state_bytes, void* stream, emb_clip_t* out);
+int emb_clip_destroy(emb_clip_t h);
+
+/* norm and factor into result[0] and result[1] (FP32 on the device).  grads: a host array of num_tensors device
+ * pointers (read during the call only), each tensor contiguous, at any alignment of its type; NULL counts as zeros.
+ * max_norm > 0, infinity for no limit.  workspace: 256-byte aligned.  Enqueue-only. */
+int emb_clip_norm(emb_clip_t h, const void* const* grads, double max_norm, float* result, void* workspace,
+                  size_t workspace_bytes, void* stream);
+/* grads[t] = grads[t] * *factor, an FP32 product rounded to the tensor's type (nearest even); nothing is written where
+ * *factor is 1.  No two tensors may share memory, nor hold `factor`.  NULL ones are left out.  Enqueue-only. */
+int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,4 +7,4 @@ bind the dense operators of ``include/emb_dense.h`` in the same library, and ``t
 trains a model on both.  Importing this package loads nothing; the bindings load the
 library on first use and raise if it has not been built.
 """
-__all__ = ["configs", "workload", "emb_cache", "mx4", "adamw", "tower"]
+__all__ = ["configs", "workload", "emb_cache", "mx4", "adamw", "rmsnorm", "w4", "clip", "tower"]

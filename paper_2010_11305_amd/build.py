@@ -21,7 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libembcache.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["k_forward.hip", "k_sort.hip", "k_update.hip", "k_small.hip", "runtime.cpp", "k_mx4.hip",
-           "k_mx4_product.hip", "k_adamw.hip", "dense.cpp"]
+           "k_mx4_product.hip", "k_adamw.hip", "k_rmsnorm.hip", "k_w4.hip", "k_w4_product.hip", "k_clip.hip", "dense.cpp",
+           "tower.cpp"]
 ARCH = "gfx950"
 
 FLAGS = [

@@ -1,0 +1,87 @@
+"""The norm of all gradients of a model together, and clipping by it (include/emb_dense.h).
+
+    clip = GradClip(params, max_norm=1.0)
+    norm, factor = clip.norm(grads)
+    opt.step(grads, grad_scale=factor)         # AdamW multiplies by it on the way
+    norm, factor = clip.clip_(grads)           # or: the gradients themselves are scaled down
+
+norm and factor stay on the GPU.
+"""
+from __future__ import annotations
+
+import ctypes
+from array import array
+
+import torch
+from torch import Tensor
+
+from . import dense_lib as lib
+
+
+class GradClip:
+    """params: tensors on one GPU whose gradients have their sizes and types (or all the type grad_dtype); any mixture of
+    float32, bfloat16 and float16.  max_norm: the largest norm, above 0 (infinity for none)."""
+
+    def __init__(self, params, max_norm: float = 1.0, grad_dtype=None):
+        params = list(params)
+        if not params or not all(p.is_cuda and p.device == params[0].device for p in params):
+            raise ValueError("params must hold at least one tensor, all on one GPU")
+        if not float(max_norm) > 0.0:
+            raise ValueError(f"max_norm must be above 0, not {max_norm}")
+        self.device, self.max_norm = params[0].device, float(max_norm)
+        n = len(params)
+        self.sizes = [p.numel() for p in params]
+        self.dtypes = [grad_dtype or p.dtype for p in params]
+        sizes, types = (ctypes.c_int64 * n)(*self.sizes), (ctypes.c_int32 * n)(*map(lib.type_of, self.dtypes))
+        c, s = lib.ClipConfig(n, 0, sizes, types), lib.ClipSizes()
+        L = lib.load()
+        lib.check(L.emb_clip_query_sizes(ctypes.byref(c), ctypes.byref(s)), "emb_clip_query_sizes")
+        self._workspace_bytes = s.workspace_bytes
+        self._state = torch.empty(max(s.state_bytes, 256), dtype=torch.uint8, device=self.device)
+        self._h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            lib.check(L.emb_clip_create(ctypes.byref(c), self._state.data_ptr(), s.state_bytes,
+                                        torch.cuda.current_stream().cuda_stream, ctypes.byref(self._h)), "emb_clip_create")
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib.load().emb_clip_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _pointers(self, grads):
+        if len(grads) != len(self.sizes):
+            raise ValueError(f"{len(grads)} gradients for {len(self.sizes)} tensors")
+        given, sizes, dtypes = grads, self.sizes, self.dtypes
+        if any(g is None for g in grads):
+            kept = [k for k, g in enumerate(grads) if g is not None]
+            given, sizes, dtypes = ([of[k] for k in kept] for of in (grads, sizes, dtypes))
+        if (list(map(Tensor.numel, given)) != sizes or not all(map(Tensor.is_contiguous, given))
+                or [g.dtype for g in given] != dtypes or not set(map(Tensor.get_device, given)) <= {self.device.index}):
+            raise ValueError(f"gradients must be contiguous, on {self.device}, and each of the size and type of its parameter")
+        return given, array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
+
+    def _norm(self, pointers):
+        result = torch.empty(2, dtype=torch.float32, device=self.device)
+        ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.device)
+        lib.call("emb_clip_norm", self.device, self._h, pointers.buffer_info()[0], self.max_norm, result.data_ptr(), ws.data_ptr(),
+                 self._workspace_bytes)
+        return result
+
+    def norm(self, grads):
+        """(norm, factor) as float32 scalars on the GPU: factor = min(1, max_norm / norm).  A gradient that is None counts as
+        zeros."""
+        return self._norm(self._pointers(list(grads))[1]).unbind()
+
+    def clip_(self, grads):
+        """norm(grads), and the gradients multiplied by the factor in place.  No two of them may share memory."""
+        given, pointers = self._pointers(list(grads))
+        result = self._norm(pointers)
+        lib.call("emb_clip_scale", self.device, self._h, pointers.buffer_info()[0], result.data_ptr() + 4)
+        lib.written(given)
+        return result.unbind()

@@ -107,6 +107,28 @@ __device__ __forceinline__ uint32_t to_bits(float x) {
   return f16_bits(x);
 }
 
+// The first n values of r to p, n <= N, whole 16-byte pieces at once.
+template <int TYPE, int N>
+__device__ __forceinline__ void store_values(typename Elem<TYPE>::type* p, int n, const Raw<TYPE, N>& r) {
+  constexpr int kPiece = 16 / Elem<TYPE>::kBytes;
+#pragma unroll
+  for (int q = 0; q < N / kPiece; ++q) {
+    if ((q + 1) * kPiece <= n) {
+      *reinterpret_cast<Bytes16*>(p + q * kPiece) = Bytes16{{r.w[4 * q], r.w[4 * q + 1], r.w[4 * q + 2], r.w[4 * q + 3]}};
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPiece; ++j) {
+        const int e = q * kPiece + j;
+        if (e >= n) continue;
+        if constexpr (TYPE == EMB_TYPE_FP32)
+          p[e] = __uint_as_float(r.w[e]);
+        else
+          p[e] = (uint16_t)(e % 2 ? r.w[e / 2] >> 16 : r.w[e / 2]);
+      }
+    }
+  }
+}
+
 // 2^(byte - 127), byte 0 .. 254 (the lowest is a subnormal number)
 __device__ __forceinline__ float power_of(uint32_t byte) {
   return __uint_as_float(byte ? byte << 23 : 0x00400000u);

@@ -1,5 +1,5 @@
-// Internal declarations of the dense operators (include/emb_dense.h): the layout of an MX4
-// matrix, shared by host and device, and the launchers.
+// Internal declarations of the dense operators (include/emb_dense.h): the layouts of MX4 and W4
+// matrices, shared by host and device, and the launchers.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -110,5 +110,112 @@ struct AdamPointers {
 hipError_t launch_adamw(const AdamDev& d, const AdamPointers& ptr, uint32_t first, int64_t part0, int64_t parts,
                         const AdamConst& c, const float* grad_scale, int param_type, int grad_type, int state_bits,
                         int rounding, hipStream_t s);
+
+// ---- Root-mean-square norm -------------------------------------------------------------------
+// A matrix argument: rows of `ld` elements.
+struct Rows {
+  const void* p;
+  int64_t ld;
+};
+
+constexpr int64_t kNormSlabRows = 256;   // rows whose part of the gain's gradient is summed in FP32
+
+struct NormForward {
+  Rows x, residual, sum, y;   // y: full-precision rows, or codes with `scales`
+  int64_t rows, cols;
+  const void* gain;
+  float* inverse;
+  float* scales;
+  float eps;
+};
+
+struct NormBackward {
+  Rows dy, h, dsum, dx;
+  int64_t rows, cols;
+  const float* inverse;
+  const void* gain;
+  void* dgain;
+  float* partial;   // [slabs][cols]
+};
+
+// gain_wide: the gain is FP32 (also where it is NULL), else of `type`.
+hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s);
+int64_t norm_slabs(int64_t rows, int64_t cols);
+hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide, hipStream_t s);
+hipError_t launch_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,
+                                   int type, int64_t ldx, hipStream_t s);
+
+// ---- 4-bit weights with group scales -----------------------------------------------------------
+// A W4 matrix in its buffer: tiles as an MX4 matrix has them, with other codes, then 16 pairs of FP16 (scale, bias) for
+// each row tile and group.
+struct W4 {
+  const uint8_t* base;
+  int64_t rows, cols;
+  int group;
+  int64_t row_tiles, col_tiles;
+  int64_t groups;   // of a row, those of the columns that pad it to whole tiles among them
+  int64_t pair_offset;
+
+  __host__ __device__ W4(const void* b, int64_t r, int64_t c, int g)
+      : base(static_cast<const uint8_t*>(b)),
+        rows(r),
+        cols(c),
+        group(g),
+        row_tiles((r + kTileRows - 1) / kTileRows),
+        col_tiles((c + kTileCols - 1) / kTileCols),
+        groups(col_tiles * (kTileCols / g)),
+        pair_offset(row_tiles * col_tiles * kTileBytes) {}
+
+  __host__ __device__ int64_t tile(int64_t rt, int64_t kt) const { return (rt * col_tiles + kt) * kTileBytes; }
+  // the pairs of the 16 rows of tile row rt for a group
+  __host__ __device__ int64_t pairs(int64_t rt, int64_t g) const { return pair_offset + (rt * groups + g) * (kTileRows * 4); }
+  __host__ __device__ int64_t bytes() const { return pair_offset + row_tiles * groups * (kTileRows * 4); }
+};
+
+hipError_t launch_w4_quantize(const void* x, int type, int64_t ld, const W4& q, hipStream_t s);
+hipError_t launch_w4_dequantize(const W4& q, void* x, int type, int64_t ld, hipStream_t s);
+hipError_t launch_w4_pack(const uint8_t* codes, const uint16_t* scales, const uint16_t* biases, const W4& q, hipStream_t s);
+hipError_t launch_w4_unpack(const W4& q, uint8_t* codes, uint16_t* scales, uint16_t* biases, hipStream_t s);
+
+struct W4Linear {
+  const void* x;
+  const float* scales;   // of 8-bit rows
+  int64_t m, ldx;
+  const float* bias;
+  void* y;
+  int64_t ldy;
+  int y_type;
+  int relu;
+};
+
+size_t w4_linear_workspace(int type, int64_t m, int64_t n, int64_t k, int group);
+hipError_t launch_w4_linear(const W4Linear& a, int type, const W4& w, void* workspace, hipStream_t s);
+
+// ---- The norm of many gradients ----------------------------------------------------------------
+constexpr int kClipThreads = 256;
+constexpr int kClipTensors = 480;   // tensors whose pointers one launch carries
+
+struct ClipTensor {
+  int64_t size;
+  int32_t type;
+  int32_t pad;
+};
+
+struct ClipPointers {
+  void* g[kClipTensors];
+};
+
+struct ClipDev {
+  const ClipTensor* tensors;
+  const AdamPart* parts;
+  int64_t chunk;   // elements of a part
+};
+
+// Squares of parts [part0, part0 + parts) of tensors from `first` on, into partial[part].
+hipError_t launch_clip_squares(const ClipDev& d, const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned parts,
+                               double* partial, hipStream_t s);
+hipError_t launch_clip_join(const double* partial, int64_t parts, double max_norm, float* result, hipStream_t s);
+hipError_t launch_clip_scale(const ClipDev& d, const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned parts,
+                             const float* factor, hipStream_t s);
 
 }  // namespace embd

@@ -44,6 +44,19 @@ class AdamwSizes(ctypes.Structure):
     ]
 
 
+class ClipConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_tensors", ctypes.c_int32),
+        ("type", ctypes.c_int32),
+        ("sizes", ctypes.POINTER(ctypes.c_int64)),
+        ("types", ctypes.POINTER(ctypes.c_int32)),
+    ]
+
+
+class ClipSizes(ctypes.Structure):
+    _fields_ = [("state_bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
+
+
 def load():
     """libembcache with the signatures of the dense operators (raises if it is not built)."""
     global _lib
@@ -71,6 +84,23 @@ def load():
         "emb_adamw_step": [P, P, P, f64, P, P],
         "emb_adamw_get_step": [P, c.POINTER(u64)],
         "emb_adamw_set_step": [P, u64],
+        "emb_rmsnorm_forward": [P, i32, i64, i64, i64, P, i64, P, i32, c.c_float, P, i64, P, i64, P, P],
+        "emb_rmsnorm_forward8": [P, i32, i64, i64, i64, P, i64, P, i32, c.c_float, P, i64, P, i64, P, P],
+        "emb_rows8_dequantize": [P, i64, i64, i64, P, P, i32, i64, P],
+        "emb_rmsnorm_backward_workspace": [i64, i64, c.POINTER(size)],
+        "emb_rmsnorm_backward": [P, i32, i64, i64, i64, P, i64, P, P, i32, P, i64, P, i64, P, P, size, P],
+        "emb_w4_query_bytes": [i64, i64, i32, c.POINTER(size)],
+        "emb_w4_quantize": [P, i32, i64, i64, i64, i32, P, P],
+        "emb_w4_dequantize": [P, i64, i64, i32, P, i32, i64, P],
+        "emb_w4_pack": [P, P, P, i64, i64, i32, P, P],
+        "emb_w4_unpack": [P, i64, i64, i32, P, P, P, P],
+        "emb_w4_linear_workspace": [i32, i64, i64, i64, i32, c.POINTER(size)],
+        "emb_w4_linear": [P, i32, P, i64, i64, i64, P, i64, i32, P, i32, P, i32, i64, P, size, P],
+        "emb_clip_query_sizes": [c.POINTER(ClipConfig), c.POINTER(ClipSizes)],
+        "emb_clip_create": [c.POINTER(ClipConfig), P, size, P, c.POINTER(P)],
+        "emb_clip_destroy": [P],
+        "emb_clip_norm": [P, P, f64, P, P, size, P],
+        "emb_clip_scale": [P, P, P, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -100,6 +130,22 @@ def call(name: str, device, *args):
         raise emb_cache.EmbCacheError(status, name)
 
 
+_bytes_of = {}
+
+
+def query(name, *dims) -> int:
+    """Buffer sizes are functions of the dimensions alone."""
+    key = (name, dims)
+    n = _bytes_of.get(key)
+    if n is None:
+        v = ctypes.c_size_t()
+        check(getattr(load(), name)(*dims, ctypes.byref(v)), name)
+        if len(_bytes_of) > 4096:
+            _bytes_of.clear()
+        n = _bytes_of[key] = v.value
+    return n
+
+
 def written(tensors):
     """Count tensors that a kernel wrote in place as changed: a backward pass that had kept one raises then, as it
     does for torch's own operations in place."""
@@ -120,6 +166,17 @@ def type_of(dtype) -> int:
     if t is None:
         raise ValueError(f"element type must be float32, bfloat16 or float16, not {dtype}")
     return t
+
+
+def result(out, rows, cols, dtype, device):
+    """(out, pointer, type, row stride) of a result [rows, cols], new where none is given."""
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=device)
+        return out, out.data_ptr(), type_of(dtype), max(cols, 1)
+    p, t, r, c, ld = matrix(out, "out")
+    if r != rows or c != cols or out.device != device:
+        raise ValueError(f"out must be [{rows}, {cols}] on {device}")
+    return out, p, t, ld
 
 
 def matrix(x, what: str):

@@ -16,26 +16,12 @@ comes out has no history, whatever went in (Linear.backward gives the gradients)
 """
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import dense_lib as lib
 
-_bytes_of = {}
-
-
-def _query(name, *dims) -> int:
-    """Buffer sizes are functions of the dimensions alone."""
-    key = (name, dims)
-    n = _bytes_of.get(key)
-    if n is None:
-        v = ctypes.c_size_t()
-        lib.check(getattr(lib.load(), name)(*dims, ctypes.byref(v)), name)
-        if len(_bytes_of) > 4096:
-            _bytes_of.clear()
-        n = _bytes_of[key] = v.value
-    return n
+_query = lib.query
+_result = lib.result
 
 
 class Mx4Matrix:
@@ -124,17 +110,6 @@ def quantize_columns(x, rounding="nearest", seed=0, step=0, out: Mx4Matrix | Non
 def quantize_both(x, rounding="nearest", seed=0, step=0, out=(None, None)):
     """(quantize(x), quantize_columns(x)) with x read once."""
     return _quantize(x, out[0], out[1], rounding, seed, step)
-
-
-def _result(out, rows, cols, dtype, device):
-    """(out, pointer, type, row stride) of a result [rows, cols], new where none is given."""
-    if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=device)
-        return out, out.data_ptr(), lib.type_of(dtype), max(cols, 1)
-    p, t, r, c, ld = lib.matrix(out, "out")
-    if r != rows or c != cols or out.device != device:
-        raise ValueError(f"out must be [{rows}, {cols}] on {device}")
-    return out, p, t, ld
 
 
 def matmul(a: Mx4Matrix, b: Mx4Matrix, dtype=torch.bfloat16, out=None):
