@@ -140,7 +140,7 @@ struct NormBackward {
 
 // gain_wide: the gain is FP32 (also where it is NULL), else of `type`.
 hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s);
-int64_t norm_slabs(int64_t rows, int64_t cols);
+int64_t norm_slabs(int64_t rows, int64_t cols, int type);
 hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide, hipStream_t s);
 hipError_t launch_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,
                                    int type, int64_t ldx, hipStream_t s);

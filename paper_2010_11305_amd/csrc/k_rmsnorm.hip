@@ -1,7 +1,8 @@
 // The root-mean-square norm of rows with the residual's addition, its output in 8 bits, and its gradients.
 //
-// Rows of any width: a workgroup takes a row and goes over it as often as it has to, a thread always over the same 8
-// columns at a time, so that what it wrote in one pass it reads in the next.
+// Rows of at most 4096 pieces of 16 bytes (and 16384 columns) stay in the registers of a team of threads, which reads and
+// writes every value once; wider ones take a workgroup a row that goes over it as often as it has to, a thread
+// always over the same 8 columns at a time, so that what it wrote in one pass it reads in the next.
 #include "dense_device.h"
 
 namespace embd {
@@ -10,6 +11,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = 8;
+template <int T>
+constexpr int kPiece = 16 / Elem<T>::kBytes;   // values of 16 bytes
 
 // The sum, and the largest, of a value over the workgroup, for every thread.  `part` is LDS of a wave's
 // number of values; it may be used again after a barrier.
@@ -46,31 +49,35 @@ __device__ __forceinline__ float inverse_of(double squares, int64_t cols, float 
   return (float)(1.0 / sqrt(squares / (double)cols + (double)eps));
 }
 
-// 8 codes of 8-bit rows at any address.
-struct __attribute__((packed, aligned(1))) Codes8 {
-  uint32_t w[2];
+// N codes of 8-bit rows at any address.
+template <int N>
+struct __attribute__((packed, aligned(1))) Codes {
+  uint32_t w[N / 4];
 };
+using Codes8 = Codes<kPer>;
 
 // What 127 stands for, over 127: not below the normal numbers, so that its reciprocal is finite.
 __device__ __forceinline__ float scale8(uint32_t amax) {
   return fmaxf(__uint_as_float(amax) / 127.0f, 0x1p-126f);
 }
 
-// 8 values to codes.  |v| <= 127.00003 scale, so nothing passes 127.
-__device__ __forceinline__ Codes8 codes8(const float (&v)[kPer], float per) {
-  Codes8 c = {{0, 0}};
+// N values to codes.  |v| <= 127.00003 scale, so nothing passes 127.
+template <int N>
+__device__ __forceinline__ Codes<N> codes_of(const float (&v)[N], float per) {
+  Codes<N> c = {};
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) c.w[j / 4] |= ((uint32_t)(int)rintf(v[j] * per) & 0xFFu) << (8 * (j % 4));
+  for (int j = 0; j < N; ++j) c.w[j / 4] |= ((uint32_t)(int)rintf(v[j] * per) & 0xFFu) << (8 * (j % 4));
   return c;
 }
 
-__device__ __forceinline__ void store_codes(int8_t* p, int n, const Codes8& c) {
-  if (n == kPer) {
-    *reinterpret_cast<Codes8*>(p) = c;
+template <int N>
+__device__ __forceinline__ void store_codes(int8_t* p, int n, const Codes<N>& c) {
+  if (n == N) {
+    *reinterpret_cast<Codes<N>*>(p) = c;
     return;
   }
 #pragma unroll
-  for (int j = 0; j < kPer; ++j)
+  for (int j = 0; j < N; ++j)
     if (j < n) p[j] = (int8_t)(c.w[j / 4] >> (8 * (j % 4)));
 }
 
@@ -105,6 +112,209 @@ __device__ __forceinline__ void load_gain(const void* gain, int64_t c, int n, fl
   load_values(static_cast<const typename Elem<GT>::type*>(gain) + c, n, r);
 #pragma unroll
   for (int j = 0; j < kPer; ++j) g[j] = r.get(j);
+}
+
+template <int TEAM>
+constexpr int kGroup = TEAM < kThreads ? kThreads : TEAM;   // threads of a workgroup of such teams
+
+// Piece k of CH of a thread t: 16 bytes from column c on.  The last piece of a row is moved back to end with it, so that every
+// access is of 16 bytes; its first `skip` values are another thread's too, which computes and writes the same.  There are
+// more than TEAM CH / 2 pieces unless CH is 1, so the first half of a thread's are whole.  (1000 x 1029 FP16 with a part of a
+// piece read value by value: 8.0 us, so 4.8.)
+struct Piece {
+  int c, skip;
+  bool in;
+};
+template <int T, int TEAM, int CH>
+__device__ __forceinline__ Piece piece_of(int64_t cols, int k, int t) {
+  const int c = (k * TEAM + t) * kPiece<T>, last = (int)cols - kPiece<T>;
+  if (k < CH / 2) return {c, 0, true};
+  return {c < last ? c : last, c < last ? 0 : c - last, c < (int)cols};
+}
+
+template <int T>
+__device__ __forceinline__ Raw<T, kPiece<T>> load_piece(const typename Elem<T>::type* p, const Piece& at) {
+  Raw<T, kPiece<T>> r = {};
+  if (at.in) {
+    const Bytes16 b = *reinterpret_cast<const Bytes16*>(p + at.c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = b.w[i];
+  }
+  return r;
+}
+template <int T>
+__device__ __forceinline__ void store_piece(typename Elem<T>::type* p, const Piece& at, const Raw<T, kPiece<T>>& r) {
+  if (at.in) *reinterpret_cast<Bytes16*>(p + at.c) = Bytes16{{r.w[0], r.w[1], r.w[2], r.w[3]}};
+}
+
+// A piece of the gain (which is FP32, or of type T).
+template <int T>
+__device__ __forceinline__ void gain_piece(const void* gain, bool wide, const Piece& at, float (&g)[kPiece<T>]) {
+  constexpr int N = kPiece<T>;
+  if (!gain) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = 1.0f;
+  } else if (T == EMB_TYPE_FP32 || wide) {
+#pragma unroll
+    for (int q = 0; q < N; q += 4) {
+      const Raw<EMB_TYPE_FP32, 4> r = load_piece<EMB_TYPE_FP32>(static_cast<const float*>(gain) + q, at);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[q + j] = r.get(j);
+    }
+  } else if constexpr (T != EMB_TYPE_FP32) {
+    const Raw<T, N> r = load_piece<T>(static_cast<const uint16_t*>(gain), at);
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = r.get(j);
+  }
+}
+
+// A row in the registers of a team, CH pieces a thread.
+template <int T, int TEAM, int CH, bool BITS8>
+__global__ __launch_bounds__(kGroup<TEAM>) void k_norm_row(NormForward a, bool gain_wide, int64_t first) {
+  constexpr int N = kPiece<T>;
+  __shared__ double sums[TEAM / 64];
+  __shared__ uint32_t tops[TEAM / 64];
+  const int t = threadIdx.x % TEAM;
+  const int64_t row = (first + blockIdx.x) * (kGroup<TEAM> / TEAM) + threadIdx.x / TEAM;
+  if (row >= a.rows) return;   // of a team that is a wave: nothing meets
+  Piece at[CH];
+  Raw<T, N> h[CH];
+  float v[CH][N];   // the gain, then y
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    at[k] = piece_of<T, TEAM, CH>(a.cols, k, t);
+    h[k] = load_piece<T>(row_of<T>(a.x, row), at[k]);
+  }
+  if (a.residual.p) {
+    Raw<T, N> r[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) r[k] = load_piece<T>(row_of<T>(a.residual, row), at[k]);
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) h[k].put(j, to_bits<T>(h[k].get(j) + r[k].get(j)));
+  }
+#pragma unroll
+  for (int k = 0; k < CH; ++k) gain_piece<T>(a.gain, gain_wide, at[k], v[k]);
+  double squares = 0.0;
+#pragma unroll
+  for (int k = 0; k < CH; ++k)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const double x = k < CH / 2 || j >= at[k].skip ? (double)h[k].get(j) : 0.0;
+      squares = fma(x, x, squares);
+    }
+  const float inverse = inverse_of(block_sum<double, TEAM>(squares, sums), a.cols, a.eps);
+  // only now, as it may lie over x and pieces overlap
+  if (a.sum.p) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) store_piece<T>(row_of<T>(a.sum, row), at[k], h[k]);
+  }
+  if (a.inverse && t == 0) a.inverse[row] = inverse;
+#pragma unroll
+  for (int k = 0; k < CH; ++k)
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[k][j] = h[k].get(j) * inverse * v[k][j];
+  if constexpr (!BITS8) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      Raw<T, N> y = {};
+#pragma unroll
+      for (int j = 0; j < N; ++j) y.put(j, to_bits<T>(v[k][j]));
+      store_piece<T>(row_of<T>(a.y, row), at[k], y);
+    }
+  } else {
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = max(top, __float_as_uint(v[k][j]) & 0x7FFFFFFFu);
+    top = block_max<TEAM>(top, tops);
+    const bool fine = top < 0x7F800000u;
+    const float scale = scale8(top), per = fine ? 1.0f / scale : 0.0f;
+    if (t == 0) a.scales[row] = fine ? scale : __uint_as_float(0x7FC00000u);
+    int8_t* out = static_cast<int8_t*>(const_cast<void*>(a.y.p)) + row * a.y.ld;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+      if (at[k].in) *reinterpret_cast<Codes<N>*>(out + at[k].c) = fine ? codes_of(v[k], per) : Codes<N>{};
+  }
+}
+
+// The gradients, rows in the registers of a team: a workgroup takes every blocks-th row (or group of rows, a team each),
+// keeps its columns' part of the gain's gradient in registers and leaves it in `partial`.
+template <int T, int TEAM, int CH>
+__global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a, bool gain_wide, int64_t first, int64_t blocks) {
+  constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM;
+  __shared__ float sums[TEAM / 64];
+  __shared__ float meet[kTeams > 1 ? kTeams - 1 : 1][kTeams > 1 ? CH * N * TEAM : 1];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  const int64_t block = first + blockIdx.x;
+  Piece at[CH];
+  float g[CH][N], sum[CH][N];
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    at[k] = piece_of<T, TEAM, CH>(a.cols, k, t);
+    gain_piece<T>(a.gain, gain_wide, at[k], g[k]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[k][j] = 0.0f;
+  }
+  const float cols = (float)a.cols;
+  for (int64_t row = block * kTeams + team; row < a.rows; row += blocks * kTeams) {
+    Raw<T, N> d[CH], h[CH], s[CH] = {};
+#pragma unroll
+    for (int k = 0; k < CH; ++k) d[k] = load_piece<T>(row_of<T>(a.dy, row), at[k]);
+#pragma unroll
+    for (int k = 0; k < CH; ++k) h[k] = load_piece<T>(row_of<T>(a.h, row), at[k]);
+    if (a.dsum.p) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) s[k] = load_piece<T>(row_of<T>(a.dsum, row), at[k]);
+    }
+    const float inverse = a.inverse[row];
+    float along = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float u = h[k].get(j) * inverse, dj = d[k].get(j);
+        along = fmaf(k < CH / 2 || j >= at[k].skip ? dj * g[k][j] : 0.0f, u, along);
+        sum[k][j] = fmaf(dj, u, sum[k][j]);
+      }
+    const float mean = block_sum<float, TEAM>(along, sums) / cols;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      Raw<T, N> out = {};
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        out.put(j, to_bits<T>((d[k].get(j) * g[k][j] - h[k].get(j) * inverse * mean) * inverse + s[k].get(j)));
+      store_piece<T>(row_of<T>(a.dx, row), at[k], out);
+    }
+  }
+  if (!a.dgain) return;
+  if constexpr (kTeams > 1) {
+    if (team) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int j = 0; j < N; ++j) meet[team - 1][(k * N + j) * TEAM + t] = sum[k][j];
+    }
+    __syncthreads();
+    if (team) return;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        for (int o = 0; o < kTeams - 1; ++o) sum[k][j] += meet[o][(k * N + j) * TEAM + t];
+  }
+  float* out = a.partial + block * a.cols;
+#pragma unroll
+  for (int k = 0; k < CH; ++k)
+#pragma unroll
+    for (int q = 0; q < N; q += 4) {
+      Raw<EMB_TYPE_FP32, 4> r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[j] = __float_as_uint(sum[k][q + j]);
+      store_piece<EMB_TYPE_FP32>(out + q, at[k], r);
+    }
 }
 
 template <int T, int GT, bool BITS8>
@@ -160,7 +370,7 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormForward a, int64_t first)
     for (int64_t c = (int64_t)threadIdx.x * kPer; c < a.cols; c += kThreads * kPer) {
       const int n = a.cols - c < kPer ? (int)(a.cols - c) : kPer;
       again(c, n, v);
-      store_codes(out + c, n, fine ? codes8(v, per) : Codes8{{0, 0}});
+      store_codes(out + c, n, fine ? codes_of(v, per) : Codes8{{0, 0}});
     }
   }
 }
@@ -218,13 +428,37 @@ __global__ __launch_bounds__(kThreads) void k_norm_gain(NormBackward a, int64_t 
   a.partial[slab * a.cols + c] = sum;
 }
 
+// The slabs' parts together: 32 columns a workgroup, 32 threads over the slabs of each.
+constexpr int kJoinCols = 32, kJoinThreads = 1024, kJoinWays = kJoinThreads / kJoinCols;
 template <int GT>
-__global__ __launch_bounds__(kThreads) void k_norm_gain_join(const float* __restrict__ partial, int64_t slabs, int64_t cols,
-                                                             typename Elem<GT>::type* __restrict__ out, int64_t first) {
-  const int64_t c = (first + blockIdx.x) * kThreads + threadIdx.x;
-  if (c >= cols) return;
+__global__ __launch_bounds__(kJoinThreads) void k_norm_gain_join(const float* __restrict__ partial, int64_t slabs, int64_t cols,
+                                                                 typename Elem<GT>::type* __restrict__ out, int64_t first) {
+  __shared__ double sums[kJoinWays / 2][kJoinCols];
+  const int col = threadIdx.x % kJoinCols, way = threadIdx.x / kJoinCols;
+  const int64_t c = (first + blockIdx.x) * kJoinCols + col;
   double sum = 0.0;
-  for (int64_t s = 0; s < slabs; ++s) sum += (double)partial[s * cols + c];
+  if (c < cols) {
+    const float* p = partial + c;
+    int64_t s = way;
+    for (; s + 7 * kJoinWays < slabs; s += 8 * kJoinWays) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p[(s + i * kJoinWays) * cols];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += (double)v[i];
+    }
+    for (; s < slabs; s += kJoinWays) sum += (double)p[s * cols];
+  }
+  // a wave holds two ways of its columns; then the first wave adds up the waves
+  sum += __shfl_xor(sum, 32);
+  if (threadIdx.x % 64 < 32) sums[threadIdx.x / 64][col] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kJoinWays / 4; ++w) sum += sums[way * (kJoinWays / 4) + w][col];
+  sum += __shfl_xor(sum, 32);
+  if (way || c >= cols) return;
   if constexpr (GT == EMB_TYPE_FP32)
     out[c] = (float)sum;
   else
@@ -256,6 +490,32 @@ __global__ __launch_bounds__(kThreads) void k_rows8_dequantize(const int8_t* __r
   store_values(x + row * ldx + c, n, out);
 }
 
+// A row that stays in registers has a whole piece and at most so many of them.
+constexpr int64_t kMostPieces = 4096, kMostCols = 16384;
+
+int64_t pieces_of(int64_t cols, int type) { return ceil_div(cols, type == EMB_TYPE_FP32 ? 4 : 8); }
+bool in_registers(int64_t cols, int type) {
+  return cols >= (type == EMB_TYPE_FP32 ? 4 : 8) && cols <= kMostCols && pieces_of(cols, type) <= kMostPieces;
+}
+
+// Calls f<TEAM, CH> for a row of so many pieces; FEW: there are so few rows that each may have a CU to itself.
+template <class F>
+hipError_t by_pieces(int64_t pieces, bool few, F f) {
+  if (few && pieces > 256) {
+    if (pieces <= 512) return f.template operator()<512, 1>();
+    if (pieces <= 1024) return f.template operator()<1024, 1>();
+    if (pieces <= 2048) return f.template operator()<1024, 2>();
+    return f.template operator()<1024, 4>();
+  }
+  if (pieces <= 64) return f.template operator()<64, 1>();
+  if (pieces <= 128) return f.template operator()<64, 2>();
+  if (pieces <= 256) return f.template operator()<64, 4>();
+  if (pieces <= 512) return f.template operator()<256, 2>();
+  if (pieces <= 1024) return f.template operator()<256, 4>();
+  if (pieces <= 2048) return f.template operator()<512, 4>();
+  return f.template operator()<512, 8>();
+}
+
 template <int T, int GT>
 hipError_t norm_as(const NormForward& a, hipStream_t s) {
   return in_launches(a.rows, kThreads, [&](int64_t first, unsigned n) {
@@ -267,47 +527,98 @@ hipError_t norm_as(const NormForward& a, hipStream_t s) {
   });
 }
 
-template <int T, int GT>
-hipError_t backward_as(const NormBackward& a, hipStream_t s) {
-  if (a.dgain) {
-    const int64_t slabs = norm_slabs(a.rows, a.cols);
-    hipError_t e = hipSuccess;
-    if (slabs)
-      e = in_launches(slabs * ceil_div(a.cols, kThreads), kThreads, [&](int64_t first, unsigned n) {
-        k_norm_gain<T><<<n, kThreads, 0, s>>>(a, first);
-        return hipGetLastError();
-      });
-    if (e != hipSuccess) return e;
-    e = in_launches(ceil_div(a.cols, kThreads), kThreads, [&](int64_t first, unsigned n) {
-      k_norm_gain_join<GT><<<n, kThreads, 0, s>>>(a.partial, slabs, a.cols, static_cast<typename Elem<GT>::type*>(a.dgain), first);
+template <int T>
+hipError_t norm_rows_as(const NormForward& a, bool gain_wide, hipStream_t s) {
+  return by_pieces(pieces_of(a.cols, T), a.rows <= 256, [&]<int TEAM, int CH>() {
+    return in_launches(ceil_div(a.rows, kGroup<TEAM> / TEAM), kGroup<TEAM>, [&](int64_t first, unsigned n) {
+      if (a.scales)
+        k_norm_row<T, TEAM, CH, true><<<n, kGroup<TEAM>, 0, s>>>(a, gain_wide, first);
+      else
+        k_norm_row<T, TEAM, CH, false><<<n, kGroup<TEAM>, 0, s>>>(a, gain_wide, first);
       return hipGetLastError();
     });
-    if (e != hipSuccess) return e;
-  }
-  if (!a.rows) return hipSuccess;
+  });
+}
+
+hipError_t join(const NormBackward& a, int64_t slabs, int type, hipStream_t s) {
+  return in_launches(ceil_div(a.cols, kJoinCols), kJoinThreads, [&](int64_t first, unsigned n) {
+#define EMBD_JOIN(GT) \
+  k_norm_gain_join<GT><<<n, kJoinThreads, 0, s>>>(a.partial, slabs, a.cols, static_cast<typename Elem<GT>::type*>(a.dgain), first)
+    if (type == EMB_TYPE_FP32)
+      EMBD_JOIN(EMB_TYPE_FP32);
+    else if (type == EMB_TYPE_BF16)
+      EMBD_JOIN(EMB_TYPE_BF16);
+    else
+      EMBD_JOIN(EMB_TYPE_FP16);
+#undef EMBD_JOIN
+    return hipGetLastError();
+  });
+}
+
+template <int T, int GT>
+hipError_t backward_as(const NormBackward& a, int64_t slabs, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.dgain)
+    e = in_launches(slabs * ceil_div(a.cols, kThreads), kThreads, [&](int64_t first, unsigned n) {
+      k_norm_gain<T><<<n, kThreads, 0, s>>>(a, first);
+      return hipGetLastError();
+    });
+  if (e != hipSuccess) return e;
   return in_launches(a.rows, kThreads, [&](int64_t first, unsigned n) {
     k_norm_dx<T, GT><<<n, kThreads, 0, s>>>(a, first);
     return hipGetLastError();
   });
 }
 
+template <int T>
+hipError_t backward_rows_as(const NormBackward& a, bool gain_wide, int64_t slabs, hipStream_t s) {
+  return by_pieces(pieces_of(a.cols, T), false, [&]<int TEAM, int CH>() {
+    return in_launches(slabs, kGroup<TEAM>, [&](int64_t first, unsigned n) {
+      k_norm_gradients<T, TEAM, CH><<<n, kGroup<TEAM>, 0, s>>>(a, gain_wide, first, slabs);
+      return hipGetLastError();
+    });
+  });
+}
+
 }  // namespace
 
-int64_t norm_slabs(int64_t rows, int64_t cols) { return ceil_div(rows, kNormSlabRows); }
+// Workgroups that share the rows, each with a part of the gain's gradient: two to a CU, but no more than have two rows a
+// team, and none with more than kNormSlabRows a team.
+int64_t norm_slabs(int64_t rows, int64_t cols, int type) {
+  if (!in_registers(cols, type)) return ceil_div(rows, kNormSlabRows);
+  const int64_t teams = pieces_of(cols, type) <= 256 ? 4 : 1;
+  const int64_t most = ceil_div(rows, 2 * teams), least = ceil_div(rows, kNormSlabRows * teams);
+  return most < 512 ? most : least > 512 ? least : 512;
+}
 
-#define EMBD_NORM_TYPES(F)                                                                \
-  switch (type) {                                                                         \
-    case EMB_TYPE_FP32:                                                                   \
-      return F<EMB_TYPE_FP32, EMB_TYPE_FP32>(a, s);                                       \
-    case EMB_TYPE_BF16:                                                                   \
-      return gain_wide ? F<EMB_TYPE_BF16, EMB_TYPE_FP32>(a, s) : F<EMB_TYPE_BF16, EMB_TYPE_BF16>(a, s); \
-    default:                                                                              \
-      return gain_wide ? F<EMB_TYPE_FP16, EMB_TYPE_FP32>(a, s) : F<EMB_TYPE_FP16, EMB_TYPE_FP16>(a, s); \
+hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s) {
+  if (in_registers(a.cols, type)) {
+    if (type == EMB_TYPE_FP32) return norm_rows_as<EMB_TYPE_FP32>(a, true, s);
+    if (type == EMB_TYPE_BF16) return norm_rows_as<EMB_TYPE_BF16>(a, gain_wide, s);
+    return norm_rows_as<EMB_TYPE_FP16>(a, gain_wide, s);
   }
+  if (type == EMB_TYPE_FP32) return norm_as<EMB_TYPE_FP32, EMB_TYPE_FP32>(a, s);
+  if (type == EMB_TYPE_BF16) return gain_wide ? norm_as<EMB_TYPE_BF16, EMB_TYPE_FP32>(a, s) : norm_as<EMB_TYPE_BF16, EMB_TYPE_BF16>(a, s);
+  return gain_wide ? norm_as<EMB_TYPE_FP16, EMB_TYPE_FP32>(a, s) : norm_as<EMB_TYPE_FP16, EMB_TYPE_FP16>(a, s);
+}
 
-hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s) { EMBD_NORM_TYPES(norm_as) }
-hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide, hipStream_t s) { EMBD_NORM_TYPES(backward_as) }
-#undef EMBD_NORM_TYPES
+hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide, hipStream_t s) {
+  const int64_t slabs = norm_slabs(a.rows, a.cols, type);
+  hipError_t e = hipSuccess;
+  if (a.rows) {
+    if (in_registers(a.cols, type))
+      e = type == EMB_TYPE_FP32   ? backward_rows_as<EMB_TYPE_FP32>(a, true, slabs, s)
+          : type == EMB_TYPE_BF16 ? backward_rows_as<EMB_TYPE_BF16>(a, gain_wide, slabs, s)
+                                  : backward_rows_as<EMB_TYPE_FP16>(a, gain_wide, slabs, s);
+    else if (type == EMB_TYPE_FP32)
+      e = backward_as<EMB_TYPE_FP32, EMB_TYPE_FP32>(a, slabs, s);
+    else if (type == EMB_TYPE_BF16)
+      e = gain_wide ? backward_as<EMB_TYPE_BF16, EMB_TYPE_FP32>(a, slabs, s) : backward_as<EMB_TYPE_BF16, EMB_TYPE_BF16>(a, slabs, s);
+    else
+      e = gain_wide ? backward_as<EMB_TYPE_FP16, EMB_TYPE_FP32>(a, slabs, s) : backward_as<EMB_TYPE_FP16, EMB_TYPE_FP16>(a, slabs, s);
+  }
+  return e == hipSuccess && a.dgain ? join(a, slabs, gain_wide ? EMB_TYPE_FP32 : type, s) : e;
+}
 
 hipError_t launch_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,
                                    int type, int64_t ldx, hipStream_t s) {

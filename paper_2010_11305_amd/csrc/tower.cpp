@@ -170,9 +170,9 @@ int emb_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_
   return status(launch_rows8_dequantize(codes, rows, cols, ldc, scales, x, type, ldx, S(stream)));
 }
 
-int emb_rmsnorm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes) {
-  if (!bytes || !norm_dims_ok(rows, cols)) return EMB_EINVAL;
-  *bytes = align_up((size_t)norm_slabs(rows, cols) * (size_t)cols * 4);
+int emb_rmsnorm_backward_workspace(int32_t type, int64_t rows, int64_t cols, size_t* bytes) {
+  if (!bytes || !type_ok(type) || !norm_dims_ok(rows, cols)) return EMB_EINVAL;
+  *bytes = align_up((size_t)norm_slabs(rows, cols, type) * (size_t)cols * 4);
   return EMB_OK;
 }
 
@@ -180,7 +180,7 @@ int emb_rmsnorm_backward(const void* dy, int32_t type, int64_t rows, int64_t col
                          const float* inverse, const void* gain, int32_t gain_type, const void* dsum, int64_t ldds, void* dx,
                          int64_t lddx, void* dgain, void* workspace, size_t workspace_bytes, void* stream) {
   size_t need = 0;
-  if (emb_rmsnorm_backward_workspace(rows, cols, &need) != EMB_OK || !type_ok(type) || !gain_ok(gain, gain_type, type) ||
+  if (emb_rmsnorm_backward_workspace(type, rows, cols, &need) != EMB_OK || !gain_ok(gain, gain_type, type) ||
       !gain_ok(dgain, gain_type, type))
     return EMB_EINVAL;
   if (!dgain) need = 0;

@@ -87,7 +87,7 @@ def load():
         "emb_rmsnorm_forward": [P, i32, i64, i64, i64, P, i64, P, i32, c.c_float, P, i64, P, i64, P, P],
         "emb_rmsnorm_forward8": [P, i32, i64, i64, i64, P, i64, P, i32, c.c_float, P, i64, P, i64, P, P],
         "emb_rows8_dequantize": [P, i64, i64, i64, P, P, i32, i64, P],
-        "emb_rmsnorm_backward_workspace": [i64, i64, c.POINTER(size)],
+        "emb_rmsnorm_backward_workspace": [i32, i64, i64, c.POINTER(size)],
         "emb_rmsnorm_backward": [P, i32, i64, i64, i64, P, i64, P, P, i32, P, i64, P, i64, P, P, size, P],
         "emb_w4_query_bytes": [i64, i64, i32, c.POINTER(size)],
         "emb_w4_quantize": [P, i32, i64, i64, i64, i32, P, P],

@@ -141,7 +141,7 @@ def backward(dy, h, inverse, gain=None, dh=None, out=None):
     need = 0
     if gain is not None:
         dgain = torch.empty(cols, dtype=gain.dtype, device=dev)
-        need = lib.query("emb_rmsnorm_backward_workspace", rows, cols)
+        need = lib.query("emb_rmsnorm_backward_workspace", t, rows, cols)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     lib.call("emb_rmsnorm_backward", dev, p, t, rows, cols, ld, hp, h_ld, inverse.data_ptr(), g, gt, s, s_ld, xp, x_ld,
              dgain.data_ptr() if gain is not None else None, ws.data_ptr() if need else None, need)

@@ -75,12 +75,13 @@ def test_rows8_refusals(L, bad):
 
 def test_norm_backward_refusals(L):
     n = ctypes.c_size_t()
-    for rows, cols in ((4, 40), (300, 1), (100000, 8192), (0, 5)):
-        assert L.emb_rmsnorm_backward_workspace(rows, cols, ctypes.byref(n)) == 0
-        assert n.value % 256 == 0 and n.value >= -(-rows // 256) * cols * 4 and n.value <= 4 * max(rows, 0) * cols + 256
-    assert L.emb_rmsnorm_backward_workspace(4, 40, None) == EINVAL
-    assert L.emb_rmsnorm_backward_workspace(4, 0, ctypes.byref(n)) == EINVAL
-    assert L.emb_rmsnorm_backward_workspace(4, 40, ctypes.byref(n)) == 0
+    for type, rows, cols in ((1, 4, 40), (0, 300, 1), (2, 100000, 8192), (1, 100000, 20000), (0, 10**6, 64), (1, 0, 5)):
+        assert L.emb_rmsnorm_backward_workspace(type, rows, cols, ctypes.byref(n)) == 0
+        # at most 4 teams of 256 rows share a part, and there are no more parts than rows
+        assert n.value % 256 == 0 and n.value >= rows // 1024 * cols * 4 and n.value <= 4 * rows * cols + 255
+    assert L.emb_rmsnorm_backward_workspace(1, 4, 40, None) == EINVAL
+    assert L.emb_rmsnorm_backward_workspace(1, 4, 0, ctypes.byref(n)) == EINVAL and L.emb_rmsnorm_backward_workspace(3, 4, 40, ctypes.byref(n)) == EINVAL
+    assert L.emb_rmsnorm_backward_workspace(1, 4, 40, ctypes.byref(n)) == 0
 
     def call(**kw):
         a = dict(dy=FAKE, type=1, rows=4, cols=40, lddy=40, h=FAR, ldh=40, inv=2 * FAR, g=3 * FAR, gt=0, ds=4 * FAR, ldds=40, dx=5 * FAR, lddx=40,
