@@ -69,28 +69,71 @@ struct Tile {
       load_values(left > 0 ? p + 32 * i : p, left > 8 ? 8 : left > 0 ? left : 0, v[i]);
     }
   }
-  __device__ __forceinline__ void operand(u32x4 (&s)[kSets]) const {
+  // 8 values of columns 32 i + .. into LDS: their parts, where `to` is set 0 and each set `pitch` (of 16 bytes) behind the one
+  // before, or as they are, the second half of FP32 ones 4 pitches behind the first
+  template <bool RAW>
+  static __device__ __forceinline__ void stage_whole(const E* p, u32x4* to, int i, int pitch) {
+    Raw<T, 8> r;
+#pragma unroll
+    for (int q = 0; q < Raw<T, 8>::kWords / 4; ++q) {
+      const Bytes16 w = *reinterpret_cast<const Bytes16*>(p + q * (16 / Elem<T>::kBytes));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[4 * q + j] = w.w[j];
+    }
+    if constexpr (RAW) {
+#pragma unroll
+      for (int q = 0; q < Raw<T, 8>::kWords / 4; ++q) to[4 * q * pitch] = u32x4{r.w[4 * q], r.w[4 * q + 1], r.w[4 * q + 2], r.w[4 * q + 3]};
+    } else {
+      u32x4 s[kParts];
+      split(r, s);
+#pragma unroll
+      for (int q = 0; q < kParts; ++q) to[(4 * q + i) * pitch] = s[q];
+    }
+  }
+  // the first n of them, zeros for the others: value by value, as it runs once
+  template <bool RAW>
+  static __device__ __forceinline__ void stage_part(const E* p, int n, u32x4* to, int i, int pitch) {
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+      Raw<T, 8> r = {};
+      r.w[0] = j < n ? load_bits<T>(p + j) : 0;
+      if constexpr (RAW) {
+        reinterpret_cast<uint32_t*>(to + j / 4 * 4 * pitch)[j % 4] = r.w[0];
+      } else {
+        u32x4 s[kParts];
+        split(r, s);
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) reinterpret_cast<uint16_t*>(&to[(4 * q + i) * pitch])[j] = (uint16_t)s[q][0];
+      }
+    }
+  }
+  // the operand of 8 values, its parts
+  static __device__ __forceinline__ void split(const Raw<T, 8>& v, u32x4 (&s)[kParts]) {
     if constexpr (T == EMB_TYPE_FP32) {
       // cut to the 8 bits of BF16 twice; what is left has 8
-      float x[4][8];
+      float x[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = __uint_as_float(v[i].w[j]);
+      for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v.w[j]);
 #pragma unroll
       for (int p = 0; p < 3; ++p)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; j += 2) {
-            const uint32_t lo = __float_as_uint(x[i][j]), hi = __float_as_uint(x[i][j + 1]);
-            s[4 * p + i][j / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-            x[i][j] -= __uint_as_float(lo & 0xFFFF0000u);
-            x[i][j + 1] -= __uint_as_float(hi & 0xFFFF0000u);
-          }
+        for (int j = 0; j < 8; j += 2) {
+          const uint32_t lo = __float_as_uint(x[j]), hi = __float_as_uint(x[j + 1]);
+          s[p][j / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+          x[j] -= __uint_as_float(lo & 0xFFFF0000u);
+          x[j + 1] -= __uint_as_float(hi & 0xFFFF0000u);
+        }
     } else {
+      s[0] = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+    }
+  }
+  __device__ __forceinline__ void operand(u32x4 (&s)[kSets]) const {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = u32x4{v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]};
+    for (int i = 0; i < 4; ++i) {
+      u32x4 p[kParts];
+      split(v[i], p);
+#pragma unroll
+      for (int q = 0; q < kParts; ++q) s[4 * q + i] = p[q];
     }
   }
 };
@@ -103,14 +146,24 @@ struct Tile<EMB_TYPE_INT8> {
   u32x2 v[4];
 
   __device__ __forceinline__ void load(const E* p) {
-    struct __attribute__((packed, aligned(1))) Bytes {
-      uint32_t w[2];
-    };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const Bytes w = *reinterpret_cast<const Bytes*>(p + 32 * i);
       v[i] = u32x2{w.w[0], w.w[1]};
     }
+  }
+  struct __attribute__((packed, aligned(1))) Bytes {
+    uint32_t w[2];
+  };
+  template <bool RAW>
+  static __device__ __forceinline__ void stage_whole(const E* p, u32x4* to, int i, int pitch) {
+    const Bytes w = *reinterpret_cast<const Bytes*>(p);
+    reinterpret_cast<u32x2*>(to + i / 2 * pitch)[i % 2] = u32x2{w.w[0], w.w[1]};
+  }
+  template <bool RAW>
+  static __device__ __forceinline__ void stage_part(const E* p, int n, u32x4* to, int i, int pitch) {
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) reinterpret_cast<uint8_t*>(reinterpret_cast<u32x2*>(to + i / 2 * pitch) + i % 2)[j] = j < n ? p[j] : 0;
   }
   __device__ __forceinline__ void load_part(const E* p, int n) {
 #pragma unroll
@@ -183,6 +236,21 @@ __device__ __forceinline__ f32x4 group_sum(const typename Tile<T>::Codes& a, con
   }
 }
 
+// Reads of a row tile's codes, or of its pairs, through a buffer descriptor: an offset past its end reads nothing and
+// gives 0, so that loops may run ahead without a branch around their loads (the compiler would wait for more than it
+// has to behind one).  Sizes stay below 2^31: at most 2^17 column tiles of 1 KB.
+struct Strip {
+  __amdgpu_buffer_rsrc_t at;
+  __device__ __forceinline__ Strip(const uint8_t* p, int bytes)
+      : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00020000)) {}
+  __device__ __forceinline__ u32x4 load4(int offset) const {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(at, offset, 0, 0));
+  }
+  __device__ __forceinline__ uint32_t load1(int offset) const { return __builtin_amdgcn_raw_buffer_load_b32(at, offset, 0, 0); }
+};
+__device__ __forceinline__ Strip codes_strip(const W4& w, int64_t rt) { return Strip(w.base + w.tile(rt, 0), (int)(w.col_tiles * kTileBytes)); }
+__device__ __forceinline__ Strip pairs_strip(const W4& w, int64_t rt) { return Strip(w.base + w.pairs(rt, 0), (int)(w.groups * kTileRows * 4)); }
+
 // What follows the sums of one output: the row's scale, bias, activation, the type.
 __device__ __forceinline__ void finish(const W4Linear& a, int64_t row, int64_t n, float v) {
   if (a.scales) v *= a.scales[row];
@@ -196,318 +264,351 @@ __device__ __forceinline__ void finish(const W4Linear& a, int64_t row, int64_t n
 }
 
 // ---- up to 16 rows -----------------------------------------------------------------------------
-// A workgroup computes 16 outputs of 16 rows; its waves (up to 16) share the column tiles.
+// A workgroup computes 16 outputs of up to 16 rows; its waves (up to 16) share the column tiles.  All of the rows are in
+// LDS, in the order of the operand; FP32 ones as they are (RAW) where their three parts would not fit.
 constexpr int kFewWaves = 16;
-// Column tiles whose loads a wave has under way at once.
-template <int T, int G>
-constexpr int kAhead = T == EMB_TYPE_FP32 || G == 32 ? 2 : G == 64 ? 3 : 4;
-
-template <int T, int G>
+constexpr int kFewLds = 65536, kFewLdsRaw = 131072;
+template <int T, int G, bool RAW>
 __global__ __launch_bounds__(64 * kFewWaves) void k_w4_few(W4Linear a, W4 w, int64_t first) {
-  constexpr int kPer = kTileCols / G, D = kAhead<T, G>;
+  constexpr int kPer = kTileCols / G, kSets = Tile<T>::kSets;
   using X = Tile<T>;
-  __shared__ f32x4 meet[kFewWaves][64];
+  extern __shared__ u32x4 lds[];
   const int lane = threadIdx.x % 64, b = lane / 16, waves = blockDim.x / 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t block = first + blockIdx.x, rt = block % w.row_tiles, row0 = block / w.row_tiles * 16;
-  const int64_t row = row0 + lane % 16;
-  // rows past the last one repeat it and are not stored
-  const typename X::E* x = static_cast<const typename X::E*>(a.x) + (row < a.m ? row : a.m - 1) * a.ldx + 8 * b;
-  const u32x4* codes = reinterpret_cast<const u32x4*>(w.base + w.tile(rt, 0)) + lane;
-  const u32x4* pairs = reinterpret_cast<const u32x4*>(w.base + w.pairs(rt, 0)) + b;
-  const int whole = (int)(w.cols / kTileCols), tail = (int)(w.cols % kTileCols);
+  const int rows = a.m - row0 < 16 ? (int)(a.m - row0) : 16, tiles = (int)w.col_tiles;
+  const int row = lane % 16 < rows ? lane % 16 : rows - 1;   // rows past the last one repeat it and are not stored
+  const auto* x = static_cast<const typename X::E*>(a.x) + row0 * a.ldx;
+  const Strip codes = codes_strip(w, rt), pairs = pairs_strip(w, rt);
+  u32x4 c, pair[kPer];
+  const auto load_w = [&](int kt) {
+    c = codes.load4(kt * kTileBytes + lane * 16);
+#pragma unroll
+    for (int g = 0; g < kPer; ++g) pair[g] = pairs.load4((kt * kPer + g) * (kTileRows * 4) + b * 16);
+  };
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  const auto add = [&](const u32x4& c, const u32x4 (&pair)[kPer], const X& rows) {
+  const auto add = [&](const u32x4 (&s)[kSets], int next) {
     typename X::Codes q;
-    u32x4 s[X::kSets];
     codes_of<T>(c, q);
-    rows.operand(s);
+    u32x4 now[kPer];
+#pragma unroll
+    for (int g = 0; g < kPer; ++g) now[g] = pair[g];
+    load_w(next);
 #pragma unroll
     for (int g = 0; g < kPer; ++g) {
       const f32x4 p = group_sum<T, G, false>(q, s, g), o = group_sum<T, G, true>(q, s, g);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        sum[r] = fmaf(f16_low(pair[g][r]), p[r], sum[r]);
-        sum[r] = fmaf(f16_high(pair[g][r]), o[r], sum[r]);
+        sum[r] = fmaf(f16_low(now[g][r]), p[r], sum[r]);
+        sum[r] = fmaf(f16_high(now[g][r]), o[r], sum[r]);
       }
     }
   };
-  for (int kt = wave; kt < whole; kt += D * waves) {
-    u32x4 c[D], pair[D][kPer];
-    X rows[D];
-#pragma unroll
-    for (int d = 0; d < D; ++d) {
-      const int64_t at = kt + d * waves < whole ? kt + d * waves : kt;   // beyond the last: loaded and not used
-      c[d] = codes[at * 64];
-#pragma unroll
-      for (int g = 0; g < kPer; ++g) pair[d][g] = pairs[(at * kPer + g) * 4];
-      rows[d].load(x + at * kTileCols);
-    }
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-      if (kt + d * waves < whole) add(c[d], pair[d], rows[d]);
+  load_w(wave);
+  // pieces of 8 columns that are whole, several loads at once; then the rest of the last tile
+  const uint32_t whole = (uint32_t)(w.cols / 8), rest = (uint32_t)tiles * 16 - whole;
+  const auto place = [&](uint32_t piece, uint32_t r) {   // of RAW, the first half of its 8 values
+    return RAW ? lds + ((piece / 16 * 8 + piece / 4 % 4) * rows + r) * 4 + piece % 4 : lds + (piece / 16 * kSets * rows + r) * 4 + piece % 4;
+  };
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < whole * rows; i += blockDim.x) {
+    const uint32_t r = i / whole, piece = i % whole;
+    X::template stage_whole<RAW>(x + r * a.ldx + 8 * piece, place(piece, r), piece / 4 % 4, rows * 4);
   }
-  if (tail && wave == whole % waves) {
-    u32x4 pair[kPer];
-#pragma unroll
-    for (int g = 0; g < kPer; ++g) pair[g] = pairs[((int64_t)whole * kPer + g) * 4];
-    X rows;
-    rows.load_part(x + (int64_t)whole * kTileCols, tail - 8 * b);
-    add(codes[(int64_t)whole * 64], pair, rows);
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < rest * rows; i += blockDim.x) {
+    const uint32_t r = i / rest, piece = whole + i % rest;
+    X::template stage_part<RAW>(x + r * a.ldx + 8 * piece, (int)w.cols - 8 * (int)piece, place(piece, r), piece / 4 % 4, rows * 4);
   }
-  meet[wave][lane] = sum;
   __syncthreads();
-  if (threadIdx.x >= 256) return;
+#pragma unroll 1
+  for (int kt = wave; kt < tiles; kt += waves) {
+    u32x4 s[kSets];
+    if constexpr (RAW) {
+      X v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 l = lds[((kt * 8 + h * 4 + i) * rows + row) * 4 + b];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v.v[i].w[4 * h + j] = l[j];
+        }
+      v.operand(s);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSets; ++i) s[i] = lds[((kt * kSets + i) * rows + row) * 4 + b];
+    }
+    add(s, kt + waves);
+  }
+  __syncthreads();   // x has been read
+  f32x4* meet = reinterpret_cast<f32x4*>(lds);
+  meet[wave * 64 + lane] = sum;
+  __syncthreads();
   // 16 outputs of a row are neighbours
   for (int t = threadIdx.x; t < 256; t += blockDim.x) {
     const int n = t % 16, r = t / 16;
     float v = 0.0f;
-    for (int k = 0; k < waves; ++k) v += meet[k][n / 4 * 16 + r][n % 4];
-    if (row0 + r < a.m && rt * 16 + n < w.rows) finish(a, row0 + r, rt * 16 + n, v);
+    for (int k = 0; k < waves; ++k) v += meet[k * 64 + n / 4 * 16 + r][n % 4];
+    if (r < rows && rt * 16 + n < w.rows) finish(a, row0 + r, rt * 16 + n, v);
   }
 }
 
-// ---- up to 64 rows -----------------------------------------------------------------------------
-// A workgroup computes 128 outputs of 16 MT rows over a share of the column tiles: two halves of four waves take them in
-// turn, each wave two row tiles of w.  A half's waves put a tile of x into LDS in the order of the operand, and with it the
-// sums of its groups, which one matrix instruction makes of the registers that are on their way there.  The halves
-// meet in LDS, the shares of the columns in the workspace.
-constexpr int kBatchWaves = 4, kBatchRows = 2, kBatchThreads = 2 * 64 * kBatchWaves;
-constexpr int kBatchOut = kBatchWaves * kBatchRows * kTileRows;   // 128
-constexpr int kCodesAhead = 3;   // iterations that the loads of codes, scales and biases run ahead
-
-template <int T>
-constexpr int kMostTiles = T == EMB_TYPE_FP32 ? 2 : 4;   // of 16 rows: FP32 rows take three times the LDS
-
-template <int T, int G, int MT>
-struct BatchStage {
-  u32x4 x[MT][Tile<T>::kSets][64];
-  float sums[MT][64];                            // of group b of the tile and row r at 16 b + r
-  uint32_t pairs[kBatchWaves][kBatchRows][64];   // (scale, bias) of group b, row r of w
+// ---- more rows -----------------------------------------------------------------------------------
+// x first goes through the workspace: tiles of 16 rows x 128 columns in the order of the operand, zeros past the last
+// column, and the sums of their groups.  Every workgroup reads all of them, whole lines at a time; rows of x lie a power
+// of two apart often enough, and then all are in one channel of the L2 (48 x 4096 x 8192 in 8 bits with x read as it lies: 26 us).
+struct Prepared {
+  u32x4* x;       // [column tile][tile of 16 rows][set][lane]
+  float* sums;    // [column tile][tile of 16 rows][lane]: of group b and row r at 16 b + r
+  int64_t tiles;  // of 16 rows
 };
+template <int T>
+Prepared prepared(void* workspace, int64_t m, const W4& w) {
+  const int64_t tiles = ceil_div(m, 16);
+  uint8_t* p = static_cast<uint8_t*>(workspace);
+  return {reinterpret_cast<u32x4*>(p), reinterpret_cast<float*>(p + w.col_tiles * tiles * Tile<T>::kSets * 1024), tiles};
+}
 
-template <int T, int G, int MT>
-__global__ __launch_bounds__(kBatchThreads) void k_w4_batch(W4Linear a, W4 w, float* __restrict__ partial, int shares, int64_t first) {
+template <int T, int G>
+__global__ __launch_bounds__(256) void k_w4_rows(W4Linear a, W4 w, Prepared out, int64_t first) {
   constexpr int kPer = kTileCols / G, kSets = Tile<T>::kSets;
   using X = Tile<T>;
-  using Stage = BatchStage<T, G, MT>;
-  __shared__ Stage stages[2][2];
-  static_assert(sizeof(stages) >= sizeof(f32x4) * kBatchWaves * kBatchRows * MT * 64);
-  const int lane = threadIdx.x % 64, b = lane / 16, r = lane % 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = wave / kBatchWaves, own = wave % kBatchWaves;
-  // shares of the same rows of w are far apart, workgroups of the same share of the columns and rows of x near: they
-  // read the same part of x
-  const int64_t block = first + blockIdx.x, wide = ceil_div(w.row_tiles, kBatchWaves * kBatchRows);
-  const int64_t nb = block % wide, share = block / wide % shares, mb = block / wide / shares;
-  const int64_t row0 = mb * MT * 16;
-  const int tiles = (int)w.col_tiles;
-  const int kt0 = (int)((int64_t)tiles * share / shares), kt1 = (int)((int64_t)tiles * (share + 1) / shares);
-  const int steps = (kt1 - kt0 + 1) / 2;
-  const int whole = (int)(w.cols / kTileCols);
-
-  // what this wave reads of w
-  int64_t rt[kBatchRows];
+  const int lane = threadIdx.x % 64, b = lane / 16;
+  const int64_t i = (first + blockIdx.x) * 4 + threadIdx.x / 64;   // a wave a tile
+  const int64_t kt = i / out.tiles, t = i % out.tiles, row = t * 16 + lane % 16;
+  if (kt >= w.col_tiles) return;
+  // rows past the last one repeat it
+  const auto* x = static_cast<const typename X::E*>(a.x) + (row < a.m ? row : a.m - 1) * a.ldx + kt * kTileCols + 8 * b;
+  X tile;
+  if ((kt + 1) * kTileCols <= w.cols)
+    tile.load(x);
+  else
+    tile.load_part(x, (int)(w.cols - kt * kTileCols) - 8 * b);
+  u32x4 s[kSets];
+  tile.operand(s);
 #pragma unroll
-  for (int i = 0; i < kBatchRows; ++i) {
-    rt[i] = (nb * kBatchWaves + own) * kBatchRows + i;
-    if (rt[i] >= w.row_tiles) rt[i] = w.row_tiles - 1;   // read again, not stored
+  for (int k = 0; k < kSets; ++k) out.x[(i * kSets + k) * 64 + lane] = s[k];
+  float total = 0.0f;
+  typename X::Codes none = {};
+#pragma unroll
+  for (int g = 0; g < kPer; ++g) {
+    const float o = group_sum<T, G, true>(none, s, g)[0];   // the same for every lane of a row
+    total = g == b ? o : total;
   }
-  u32x4 codes[kCodesAhead][kBatchRows];
-  uint32_t pairs[kCodesAhead][kBatchRows];
-  const auto tile_of = [&](int step) {
-    const int kt = kt0 + 2 * step + half;
-    return kt < kt1 ? kt : kt1 - 1;   // beyond the last: loaded and not used
-  };
-  const auto load_w = [&](int step, u32x4 (&c)[kBatchRows], uint32_t (&p)[kBatchRows]) {
-    const int kt = tile_of(step);
-#pragma unroll
-    for (int i = 0; i < kBatchRows; ++i) {
-      c[i] = reinterpret_cast<const u32x4*>(w.base + w.tile(rt[i], kt))[lane];
-      p[i] = reinterpret_cast<const uint32_t*>(w.base + w.pairs(rt[i], (int64_t)kt * kPer))[lane % (16 * kPer)];
-    }
-  };
-  // the tile of x that this wave puts into LDS, of rows own, own + 4, .. (MT is at most 4: one, or none)
-  const bool brings = own < MT;
-  const int64_t row = row0 + own * 16 + r;
-  const typename X::E* x = static_cast<const typename X::E*>(a.x) + (row < a.m ? row : a.m - 1) * a.ldx + 8 * b;
-  X rows;
-  const auto load_x = [&](int step) {
-    if (!brings) return;
-    const int kt = tile_of(step);
-    if (kt < whole)
-      rows.load(x + (int64_t)kt * kTileCols);
-    else
-      rows.load_part(x + (int64_t)kt * kTileCols, (int)(w.cols - (int64_t)kt * kTileCols) - 8 * b);
-  };
-  f32x4 sum[kBatchRows][MT] = {};
-  load_x(0);
-#pragma unroll
-  for (int s = 0; s < kCodesAhead; ++s) load_w(s, codes[s], pairs[s]);
-  const auto step = [&](int it, u32x4 (&c)[kBatchRows], uint32_t (&p)[kBatchRows]) {
-    Stage& st = stages[half][it % 2];
-    if (brings) {
-      u32x4 s[kSets];
-      rows.operand(s);
-#pragma unroll
-      for (int i = 0; i < kSets; ++i) st.x[own][i][lane] = s[i];
-      float total = 0.0f;
-      typename X::Codes none = {};
-#pragma unroll
-      for (int g = 0; g < kPer; ++g) {
-        const float o = group_sum<T, G, true>(none, s, g)[0];   // the same for every lane of a row
-        total = g == b ? o : total;
-      }
-      st.sums[own][lane] = total;
-    }
-#pragma unroll
-    for (int i = 0; i < kBatchRows; ++i) st.pairs[own][i][lane] = p[i];
-    typename X::Codes q[kBatchRows];
-#pragma unroll
-    for (int i = 0; i < kBatchRows; ++i) codes_of<T>(c[i], q[i]);
-    load_x(it + 1);
-    load_w(it + kCodesAhead, c, p);
-    __syncthreads();
-    if (kt0 + 2 * it + half >= kt1) return;
-    // bias * sum(x) of up to four groups is one FP32 matrix instruction
-    float bias[kBatchRows];
-#pragma unroll
-    for (int i = 0; i < kBatchRows; ++i) bias[i] = b < kPer ? f16_high(st.pairs[own][i][lane]) : 0.0f;
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      u32x4 s[kSets];
-#pragma unroll
-      for (int i = 0; i < kSets; ++i) s[i] = st.x[t][i][lane];
-      const float ones = st.sums[t][lane];
-#pragma unroll
-      for (int i = 0; i < kBatchRows; ++i) {
-        sum[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(bias[i], ones, sum[i][t], 0, 0, 0);
-#pragma unroll
-        for (int g = 0; g < kPer; ++g) {
-          const f32x4 v = group_sum<T, G, false>(q[i], s, g);
-          const u32x4 pair = *reinterpret_cast<const u32x4*>(&st.pairs[own][i][16 * g + 4 * b]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sum[i][t][k] = fmaf(f16_low(pair[k]), v[k], sum[i][t][k]);
-        }
-      }
-    }
-  };
-  for (int it = 0; it < steps; it += kCodesAhead) {
-#pragma unroll
-    for (int s = 0; s < kCodesAhead; ++s)
-      if (it + s < steps) step(it + s, codes[s], pairs[s]);
-  }
-  __syncthreads();
-  f32x4* meet = reinterpret_cast<f32x4*>(&stages[0][0]);
-  const auto place = [&](int i, int t) { return ((own * kBatchRows + i) * MT + t) * 64 + lane; };
-  if (half) {
-#pragma unroll
-    for (int i = 0; i < kBatchRows; ++i)
-#pragma unroll
-      for (int t = 0; t < MT; ++t) meet[place(i, t)] = sum[i][t];
-  }
-  __syncthreads();
-  if (half) return;
-#pragma unroll
-  for (int i = 0; i < kBatchRows; ++i) {
-    const int64_t n = ((nb * kBatchWaves + own) * kBatchRows + i) * 16 + 4 * b;
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const f32x4 v = sum[i][t] + meet[place(i, t)];
-      const int64_t m = row0 + t * 16 + r;
-      if (m >= a.m || n >= w.rows) continue;
-      if (shares > 1) {
-        // rows of whole row tiles: four outputs at once
-        *reinterpret_cast<f32x4*>(partial + (share * a.m + m) * w.row_tiles * 16 + n) = v;
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (n + k < w.rows) finish(a, m, n + k, v[k]);
-      }
-    }
-  }
+  out.sums[i * 64 + lane] = total;
 }
 
-// The shares' sums together: four outputs a thread.
-__global__ __launch_bounds__(256) void k_w4_join(W4Linear a, W4 w, const float* __restrict__ partial, int shares, int64_t first) {
-  const int64_t wide = w.row_tiles * 4, i = (first + blockIdx.x) * 256 + threadIdx.x, m = i / wide, n = i % wide * 4;
-  if (m >= a.m || n >= w.rows) return;
-  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  const f32x4* p = reinterpret_cast<const f32x4*>(partial) + i;
-#pragma unroll 4
-  for (int s = 0; s < shares; ++s) v += p[s * a.m * wide];
+// A workgroup computes 16 RT outputs of 16 MT rows; its waves share the column tiles.  No wave waits for another before the
+// end, and no sums leave the workgroup.
+template <int T>
+constexpr int kMostTiles = T == EMB_TYPE_FP32 ? 2 : 4;   // of 16 rows: an operand of FP32 rows takes three times the registers
+template <int RT>
+constexpr int kMoreWaves = RT == 2 ? 12 : 16;            // 168 registers a wave, or 128
+
+struct WavePairs {       // scales and biases of a wave's tile, in LDS
+  uint16_t scales[64];   // of group g of the tile and row r of w at 16 g + r
+  uint16_t biases[64];
+};
+
+template <int T, int G, int MT, int RT>
+__global__ __launch_bounds__(64 * kMoreWaves<RT>) void k_w4_more(W4Linear a, W4 w, Prepared in, int64_t first) {
+  constexpr int kPer = kTileCols / G, kSets = Tile<T>::kSets;
+  constexpr int kRing = kSets <= 4 && MT > 1 ? 2 : 1;   // operands under way
+  constexpr bool kBiasByMatrix = G < 128;   // up to four groups are one FP32 matrix instruction; one is less by itself
+  extern __shared__ u32x4 lds[];
+  const int lane = threadIdx.x % 64, b = lane / 16, waves = blockDim.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t block = first + blockIdx.x, wide = ceil_div(w.row_tiles, RT), rt0 = block % wide * RT, t0 = block / wide * MT;
+  const int tiles = (int)w.col_tiles;
+  WavePairs* mine = reinterpret_cast<WavePairs*>(lds) + wave * RT;
+  // tiles past the last one repeat it and are not stored, of x and of w
+  int64_t at[MT];
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (n + k < w.rows) finish(a, m, n + k, v[k]);
+  for (int t = 0; t < MT; ++t) at[t] = t0 + t < in.tiles ? t0 + t : in.tiles - 1;
+  u32x4 c[RT];
+  uint32_t p[RT];
+  const auto strip_of = [&](int i) { return rt0 + i < w.row_tiles ? rt0 + i : w.row_tiles - 1; };
+  const auto load_w = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      p[i] = pairs_strip(w, strip_of(i)).load1((kt * kPer * 16 + lane % (16 * kPer)) * 4);
+      c[i] = codes_strip(w, strip_of(i)).load4(kt * kTileBytes + lane * 16);
+    }
+  };
+  f32x4 sum[RT][MT] = {};
+  load_w(wave);
+#pragma unroll 1
+  for (int kt = wave; kt < tiles; kt += waves) {
+    u32x4 s[kRing][kSets];
+    float ones[MT];
+    const auto load_x = [&](int t) {
+      const int64_t i = kt * in.tiles + at[t];
+#pragma unroll
+      for (int k = 0; k < kSets; ++k) s[t % kRing][k] = in.x[(i * kSets + k) * 64 + lane];
+    };
+#pragma unroll
+    for (int t = 0; t < MT; ++t) ones[t] = in.sums[(kt * in.tiles + at[t]) * 64 + (kBiasByMatrix ? lane : lane % 16)];
+#pragma unroll
+    for (int t = 0; t < kRing; ++t) load_x(t);
+    typename Tile<T>::Codes q[RT];
+    float bias[RT];
+    u32x2 scale[RT][kPer], one_bias[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      mine[i].scales[lane] = (uint16_t)p[i];
+      mine[i].biases[lane] = (uint16_t)(p[i] >> 16);
+      bias[i] = b < kPer ? f16_high(p[i]) : 0.0f;
+      codes_of<T>(c[i], q[i]);
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+#pragma unroll
+      for (int g = 0; g < kPer; ++g) scale[i][g] = *reinterpret_cast<const u32x2*>(&mine[i].scales[16 * g + 4 * b]);
+      one_bias[i] = *reinterpret_cast<const u32x2*>(&mine[i].biases[4 * b]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (MT <= kRing) load_w(kt + waves);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      // loads return in order: those of w, from farther away, go last
+      const auto next = [&] {
+        if (t + kRing < MT) load_x(t + kRing);
+        if (t + kRing == MT - 1) load_w(kt + waves);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        if constexpr (kBiasByMatrix) {
+          sum[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(bias[i], ones[t], sum[i][t], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            sum[i][t][k] = fmaf(k % 2 ? f16_high(one_bias[i][k / 2]) : f16_low(one_bias[i][k / 2]), ones[t], sum[i][t][k]);
+        }
+#pragma unroll
+        for (int g = 0; g < kPer; ++g) {
+          const f32x4 v = group_sum<T, G, false>(q[i], s[t % kRing], g);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            sum[i][t][k] = fmaf(k % 2 ? f16_high(scale[i][g][k / 2]) : f16_low(scale[i][g][k / 2]), v[k], sum[i][t][k]);
+        }
+      }
+      next();
+    }
+  }
+  __syncthreads();   // scales and biases have been read
+  f32x4* meet = reinterpret_cast<f32x4*>(lds);
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) meet[((wave * RT + i) * MT + t) * 64 + lane] = sum[i][t];
+  __syncthreads();
+  // 16 RT outputs of a row are neighbours
+  for (int i = threadIdx.x; i < 256 * RT * MT; i += blockDim.x) {
+    const int n = i % (16 * RT), m = i / (16 * RT);
+    const f32x4* from = meet + ((n / 16) * MT + m / 16) * 64 + n % 16 / 4 * 16 + m % 16;
+    float v = 0.0f;
+    for (int k = 0; k < waves; ++k) v += from[k * RT * MT * 64][n % 4];
+    if (t0 * 16 + m < a.m && rt0 * 16 + n < w.rows) finish(a, t0 * 16 + m, rt0 * 16 + n, v);
+  }
 }
 
 // ---- which of them -----------------------------------------------------------------------------
-bool few(int64_t m) { return m <= 16; }
-
-// Shares of the columns: as many workgroups as there are CUs, each with two tiles at least for either half.
-int batch_shares(int64_t m, int64_t n, int64_t k, int most_tiles) {
-  const int64_t blocks = ceil_div(ceil_div(n, 16), kBatchWaves * kBatchRows) * ceil_div(m, 16 * most_tiles);
-  const int64_t tiles = ceil_div(k, kTileCols), want = 256 / blocks, most = tiles / 4;
-  const int64_t s = want < most ? want : most;
-  return s < 1 ? 1 : (int)s;
+template <int T, int G, int MT, int RT>
+hipError_t more_as(const W4Linear& a, const W4& w, const Prepared& in, hipStream_t s) {
+  int waves = 4;   // of those that have a column tile
+  while (waves < kMoreWaves<RT> && waves < w.col_tiles) waves += 4;
+  return in_launches(ceil_div(w.row_tiles, RT) * ceil_div(in.tiles, MT), 64 * waves, [&](int64_t first, unsigned n) {
+    k_w4_more<T, G, MT, RT><<<n, 64 * waves, waves * RT * MT * 1024, s>>>(a, w, in, first);
+    return hipGetLastError();
+  });
 }
-int most_tiles(int type) { return type == EMB_TYPE_FP32 ? kMostTiles<EMB_TYPE_FP32> : kMostTiles<EMB_TYPE_BF16>; }
 
 template <int T, int G, int MT>
-hipError_t batch_as(const W4Linear& a, const W4& w, float* partial, int shares, hipStream_t s) {
-  const int64_t blocks = ceil_div(w.row_tiles, kBatchWaves * kBatchRows) * shares * ceil_div(a.m, 16 * MT);
-  return in_launches(blocks, kBatchThreads, [&](int64_t first, unsigned n) {
-    k_w4_batch<T, G, MT><<<n, kBatchThreads, 0, s>>>(a, w, partial, shares, first);
+hipError_t more_of(const W4Linear& a, const W4& w, const Prepared& in, hipStream_t s) {
+  // 32 outputs a workgroup, and x read half as often, where that still is a workgroup for every CU
+  return w.row_tiles * ceil_div(in.tiles, MT) >= 512 ? more_as<T, G, MT, 2>(a, w, in, s) : more_as<T, G, MT, 1>(a, w, in, s);
+}
+
+// Bytes of LDS that x takes in k_w4_few (of a block of 16 rows where there are more); as it is: of FP32 rows.
+template <int T>
+int64_t few_bytes(int64_t m, int64_t k, bool raw) {
+  return (m < 16 ? m : 16) * ceil_div(k, kTileCols) * (raw ? 512 : Tile<T>::kSets * 64);
+}
+template <int T>
+bool few_raw(int64_t m, int64_t k) { return T == EMB_TYPE_FP32 && few_bytes<T>(m, k, false) > kFewLds; }
+// Whether k_w4_few takes a product.
+template <int T>
+bool few(int64_t m, int64_t n, int64_t k) {
+  const bool raw = few_raw<T>(m, k);
+  if (few_bytes<T>(m, k, raw) > (raw ? kFewLdsRaw : kFewLds)) return false;
+  // the weight is read for each 16 rows; us (BF16, the other way): 64 x 2048 x 2048 7.5 (9.3), 64 x 8192 x 512 7.7 (9.4),
+  // 32 x 8192 x 2048 15.1 (9.0)
+  return m <= 16 || ceil_div(m, 16) * ceil_div(n, 16) * ceil_div(k, kTileCols) <= 8192;
+}
+
+template <int T, int G>
+hipError_t few_as(const W4Linear& a, const W4& w, hipStream_t s) {
+  int waves = 4;   // enough to fill the CUs, of those that have a column tile
+  const int64_t blocks = w.row_tiles * ceil_div(a.m, 16);
+  while (waves < kFewWaves && waves < w.col_tiles && waves * blocks < 256 * kFewWaves) waves *= 2;
+  const bool raw = few_raw<T>(a.m, w.cols);
+  const int64_t x_bytes = few_bytes<T>(a.m, w.cols, raw), meet = waves * 1024;
+  const size_t bytes = (size_t)(x_bytes > meet ? x_bytes : meet);
+  return in_launches(blocks, 64 * waves, [&](int64_t first, unsigned n) {
+    if constexpr (T == EMB_TYPE_FP32) {
+      if (raw) {
+        k_w4_few<T, G, true><<<n, 64 * waves, bytes, s>>>(a, w, first);
+        return hipGetLastError();
+      }
+    }
+    k_w4_few<T, G, false><<<n, 64 * waves, bytes, s>>>(a, w, first);
     return hipGetLastError();
   });
 }
 
 template <int T, int G>
-hipError_t linear_as(const W4Linear& a, const W4& w, float* partial, hipStream_t s) {
-  if (few(a.m) || !w.cols) {
-    int waves = 4;   // enough to fill the CUs, of those that have a column tile
-    while (waves < kFewWaves && waves < w.col_tiles && waves * w.row_tiles < 256 * kFewWaves) waves *= 2;
-    return in_launches(w.row_tiles * ceil_div(a.m, 16), 64 * waves, [&](int64_t first, unsigned n) {
-      k_w4_few<T, G><<<n, 64 * waves, 0, s>>>(a, w, first);
-      return hipGetLastError();
-    });
-  }
-  const int shares = batch_shares(a.m, w.rows, w.cols, kMostTiles<T>);
-  const int64_t tiles = ceil_div(a.m, 16);
-  hipError_t e;
-  if (tiles <= 2 || kMostTiles<T> == 2)
-    e = batch_as<T, G, 2>(a, w, partial, shares, s);
-  else if (tiles == 3)
-    e = batch_as<T, G, kMostTiles<T> == 2 ? 2 : 3>(a, w, partial, shares, s);
-  else
-    e = batch_as<T, G, kMostTiles<T>>(a, w, partial, shares, s);
-  if (e != hipSuccess || shares == 1) return e;
-  return in_launches(ceil_div(a.m * w.row_tiles * 4, 256), 256, [&](int64_t first, unsigned n) {
-    k_w4_join<<<n, 256, 0, s>>>(a, w, partial, shares, first);
+hipError_t linear_as(const W4Linear& a, const W4& w, void* workspace, hipStream_t s) {
+  if (few<T>(a.m, w.rows, w.cols)) return few_as<T, G>(a, w, s);
+  const Prepared in = prepared<T>(workspace, a.m, w);
+  const hipError_t e = in_launches(ceil_div(w.col_tiles * in.tiles, 4), 256, [&](int64_t first, unsigned n) {
+    k_w4_rows<T, G><<<n, 256, 0, s>>>(a, w, in, first);
     return hipGetLastError();
   });
+  if (e != hipSuccess) return e;
+  if (in.tiles == 1) return more_of<T, G, 1>(a, w, in, s);
+  if (in.tiles == 2 || kMostTiles<T> == 2) return more_of<T, G, 2>(a, w, in, s);
+  if constexpr (kMostTiles<T> > 2) return in.tiles == 3 ? more_of<T, G, 3>(a, w, in, s) : more_of<T, G, 4>(a, w, in, s);
+  return hipErrorInvalidValue;
 }
 
 template <int T>
-hipError_t linear_of(const W4Linear& a, const W4& w, float* partial, hipStream_t s) {
-  if (w.group == 32) return linear_as<T, 32>(a, w, partial, s);
-  if (w.group == 64) return linear_as<T, 64>(a, w, partial, s);
-  return linear_as<T, 128>(a, w, partial, s);
+hipError_t linear_of(const W4Linear& a, const W4& w, void* workspace, hipStream_t s) {
+  if (w.group == 32) return linear_as<T, 32>(a, w, workspace, s);
+  if (w.group == 64) return linear_as<T, 64>(a, w, workspace, s);
+  return linear_as<T, 128>(a, w, workspace, s);
+}
+
+template <int T>
+size_t workspace_of(int64_t m, int64_t n, int64_t k) {
+  return few<T>(m, n, k) ? 0 : (size_t)(ceil_div(k, kTileCols) * ceil_div(m, 16)) * (Tile<T>::kSets * 1024 + 256);
 }
 
 }  // namespace
 
 size_t w4_linear_workspace(int type, int64_t m, int64_t n, int64_t k, int group) {
-  if (few(m)) return 0;
-  const int shares = batch_shares(m, n, k, most_tiles(type));
-  return shares > 1 ? (size_t)shares * (size_t)m * (size_t)ceil_div(n, 16) * 16 * 4 : 0;
+  if (type == EMB_TYPE_FP32) return workspace_of<EMB_TYPE_FP32>(m, n, k);
+  if (type == EMB_TYPE_INT8) return workspace_of<EMB_TYPE_INT8>(m, n, k);
+  return workspace_of<EMB_TYPE_BF16>(m, n, k);
 }
 
 hipError_t launch_w4_linear(const W4Linear& a, int type, const W4& w, void* workspace, hipStream_t s) {
-  float* partial = static_cast<float*>(workspace);
-  if (type == EMB_TYPE_FP32) return linear_of<EMB_TYPE_FP32>(a, w, partial, s);
-  if (type == EMB_TYPE_BF16) return linear_of<EMB_TYPE_BF16>(a, w, partial, s);
-  if (type == EMB_TYPE_FP16) return linear_of<EMB_TYPE_FP16>(a, w, partial, s);
-  return linear_of<EMB_TYPE_INT8>(a, w, partial, s);
+  if (type == EMB_TYPE_FP32) return linear_of<EMB_TYPE_FP32>(a, w, workspace, s);
+  if (type == EMB_TYPE_BF16) return linear_of<EMB_TYPE_BF16>(a, w, workspace, s);
+  if (type == EMB_TYPE_FP16) return linear_of<EMB_TYPE_FP16>(a, w, workspace, s);
+  return linear_of<EMB_TYPE_INT8>(a, w, workspace, s);
 }
 
 }  // namespace embd

@@ -306,3 +306,59 @@ def test_graph_and_streams(torch):
     want = graphs[0][2]()
     torch.cuda.synchronize()
     assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+LARGE = [(16, 33, 8200), (16, 8200, 8200), (17, 4000, 2200), (20, 8200, 1200), (40, 3000, 2100), (48, 8177, 700), (64, 2100, 2100), (70, 8200, 520), (7, 50, 4100),
+         (200, 1700, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16", "int8"])
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("m,n,k", LARGE)
+def test_exact_products_of_large_ones(torch, m, n, k, group, dtype):
+    """The routes of large products (one block of 16 rows to four of them, one row tile of the weight and two), of whole numbers
+    whose sums stay below 2^24: every element is exact."""
+    from paper_2010_11305_amd import w4
+    from paper_2010_11305_amd.rmsnorm import Rows8
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + n + k + group)
+    rand = lambda lo, hi, *shape: torch.randint(lo, hi, shape, generator=g, device="cuda")  # noqa: E731
+    groups = -(-k // group)
+    codes, scales, biases = rand(0, 16, n, k + k % 2), rand(1, 4, n, groups), rand(-20, 1, n, groups)
+    w = w4.from_codes((codes[:, 0::2] + 16 * codes[:, 1::2]).to(torch.uint8), scales.half(), biases.half(), k, group)
+    at = torch.arange(k, device="cuda") // group
+    W = (codes[:, :k] * scales[:, at] + biases[:, at]).double()
+    X = rand(-8, 9, m, k)
+    x = Rows8(X.to(torch.int8), torch.full((m,), 0.5, device="cuda")) if dtype == "int8" else X.to(DTYPES[dtype])
+    want = X.double() @ W.t() * (0.5 if dtype == "int8" else 1.0)
+    out = torch.full((m, n + 3), 7.0, device="cuda")
+    w4.linear(x, w, out=out[:, 1:n + 1])
+    assert torch.equal(out[:, 1:n + 1].double(), want) and (out[:, 0] == 7).all() and (out[:, n + 1:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "int8"])
+def test_large_products(torch, dtype):
+    """Values of all magnitudes through the same routes, with bias and activation; what is not finite stays in its row."""
+    from paper_2010_11305_amd import w4
+    from paper_2010_11305_amd.rmsnorm import Rows8
+
+    for m, n, k, group in ((16, 300, 8200, 64), (33, 2500, 2200, 32), (64, 8200, 700, 128)):
+        parts = ref.w4_quantize(weight(n, k, 3), group)
+        w = w4.from_codes(*(torch.from_numpy(v).cuda() for v in (ref.pack(parts[0]), *parts[1:])), k, group)
+        x, X = rows_of(torch, m, k, dtype, 9)
+        b = torch.from_numpy(np.random.default_rng(m).standard_normal(n)).float().cuda()
+        y = w4.linear(x, w, bias=b, relu=True, dtype=torch.float32)
+        check(torch, y, X, parts, group, dtype, "fp32", f64(b), True)
+        wide = torch.zeros((m, k + 5), dtype=(x.codes if dtype == "int8" else x).dtype, device="cuda")
+        wide[:, 3:k + 3].copy_(x.codes if dtype == "int8" else x)
+        inside = wide[:, 3:k + 3]
+        again = w4.linear(Rows8(inside, x.scales) if dtype == "int8" else inside, w, bias=b, relu=True, dtype=torch.float32)
+        assert torch.equal(again, y)
+        if dtype == "int8":
+            x.scales[2] = float("nan")
+        else:
+            x[2, k - 1] = float("nan")
+        z = w4.linear(x, w, bias=b, relu=True, dtype=torch.float32)
+        keep = [i for i in range(m) if i != 2]
+        assert torch.isnan(z[2]).all() and torch.equal(z[keep], y[keep])
