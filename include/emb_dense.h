@@ -330,6 +330,10 @@ int emb_clip_norm(emb_clip_t h, const void* const* grads, double max_norm, float
 /* grads[t] = grads[t] * *factor, an FP32 product rounded to the tensor's type (nearest even); nothing is written where
  * *factor is 1.  No two tensors may share memory, nor hold `factor`.  NULL ones are left out.  Enqueue-only. */
 int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* stream);
+/* Both: norm and factor into `result`, and the gradients multiplied by the factor.  No two tensors may share memory, nor
+ * hold `result`.  Enqueue-only. */
+int emb_clip_apply(emb_clip_t h, void* const* grads, double max_norm, float* result, void* workspace,
+                   size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

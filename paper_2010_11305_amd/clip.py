@@ -11,11 +11,14 @@ from __future__ import annotations
 
 import ctypes
 from array import array
+from operator import attrgetter
 
 import torch
 from torch import Tensor
 
 from . import dense_lib as lib
+
+dtype_of = attrgetter("dtype")
 
 
 class GradClip:
@@ -55,33 +58,40 @@ class GradClip:
             pass
 
     def _pointers(self, grads):
+        """(the gradients that are there, an array of all addresses)"""
         if len(grads) != len(self.sizes):
             raise ValueError(f"{len(grads)} gradients for {len(self.sizes)} tensors")
         given, sizes, dtypes = grads, self.sizes, self.dtypes
-        if any(g is None for g in grads):
+        if type(None) in set(map(type, grads)):
             kept = [k for k, g in enumerate(grads) if g is not None]
             given, sizes, dtypes = ([of[k] for k in kept] for of in (grads, sizes, dtypes))
         if (list(map(Tensor.numel, given)) != sizes or not all(map(Tensor.is_contiguous, given))
-                or [g.dtype for g in given] != dtypes or not set(map(Tensor.get_device, given)) <= {self.device.index}):
+                or list(map(dtype_of, given)) != dtypes or not set(map(Tensor.get_device, given)) <= {self.device.index}):
             raise ValueError(f"gradients must be contiguous, on {self.device}, and each of the size and type of its parameter")
         return given, array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
-
-    def _norm(self, pointers):
-        result = torch.empty(2, dtype=torch.float32, device=self.device)
-        ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.device)
-        lib.call("emb_clip_norm", self.device, self._h, pointers.buffer_info()[0], self.max_norm, result.data_ptr(), ws.data_ptr(),
-                 self._workspace_bytes)
-        return result
 
     def norm(self, grads):
         """(norm, factor) as float32 scalars on the GPU: factor = min(1, max_norm / norm).  A gradient that is None counts as
         zeros."""
-        return self._norm(self._pointers(list(grads))[1]).unbind()
+        result = torch.empty(2, dtype=torch.float32, device=self.device)
+        pointers = self._pointers(list(grads))[1]
+        lib.call_in("emb_clip_norm", self.device, self._workspace_bytes, self._h, pointers.buffer_info()[0], self.max_norm,
+                    result.data_ptr())
+        return result.unbind()
 
     def clip_(self, grads):
         """norm(grads), and the gradients multiplied by the factor in place.  No two of them may share memory."""
+        result = torch.empty(2, dtype=torch.float32, device=self.device)
         given, pointers = self._pointers(list(grads))
-        result = self._norm(pointers)
-        lib.call("emb_clip_scale", self.device, self._h, pointers.buffer_info()[0], result.data_ptr() + 4)
+        lib.call_in("emb_clip_apply", self.device, self._workspace_bytes, self._h, pointers.buffer_info()[0], self.max_norm,
+                    result.data_ptr())
         lib.written(given)
         return result.unbind()
+
+    def scale_(self, grads, factor):
+        """The gradients multiplied in place by a float32 scalar on the GPU (a factor that several processes agreed on, say)."""
+        if factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != self.device:
+            raise ValueError(f"factor must be one float32 value on {self.device}")
+        given, pointers = self._pointers(list(grads))
+        lib.call("emb_clip_scale", self.device, self._h, pointers.buffer_info()[0], factor.data_ptr())
+        lib.written(given)

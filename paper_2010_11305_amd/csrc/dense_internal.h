@@ -140,7 +140,9 @@ struct NormBackward {
 
 // gain_wide: the gain is FP32 (also where it is NULL), else of `type`.
 hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s);
+// Parts of the gain's gradient in the workspace; one of rows in registers goes without.
 int64_t norm_slabs(int64_t rows, int64_t cols, int type);
+bool norm_in_registers(int64_t cols, int type);
 hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide, hipStream_t s);
 hipError_t launch_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,
                                    int type, int64_t ldx, hipStream_t s);
@@ -215,6 +217,9 @@ struct ClipDev {
 hipError_t launch_clip_squares(const ClipDev& d, const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned parts,
                                double* partial, hipStream_t s);
 hipError_t launch_clip_join(const double* partial, int64_t parts, double max_norm, float* result, hipStream_t s);
+// Joins all parts and scales parts [part0, part0 + some); the launch that holds part 0 writes the result.
+hipError_t launch_clip_join_scale(const ClipDev& d, const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some,
+                                  const double* partial, int64_t parts, double max_norm, float* result, hipStream_t s);
 hipError_t launch_clip_scale(const ClipDev& d, const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned parts,
                              const float* factor, hipStream_t s);
 

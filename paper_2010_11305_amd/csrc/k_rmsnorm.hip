@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_row(NormForward a, bool g
 }
 
 // The gradients, rows in the registers of a team: a workgroup takes every blocks-th row (or group of rows, a team each),
-// keeps its columns' part of the gain's gradient in registers and leaves it in `partial`.
+// keeps its columns' part of the gain's gradient in registers and leaves it in `partial` (a single one: in `dgain`).
 template <int T, int TEAM, int CH>
 __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a, bool gain_wide, int64_t first, int64_t blocks) {
   constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM;
@@ -305,7 +305,17 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
       for (int j = 0; j < N; ++j)
         for (int o = 0; o < kTeams - 1; ++o) sum[k][j] += meet[o][(k * N + j) * TEAM + t];
   }
-  float* out = a.partial + block * a.cols;
+  if (T != EMB_TYPE_FP32 && !gain_wide && blocks == 1) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      Raw<T, N> r = {};
+#pragma unroll
+      for (int j = 0; j < N; ++j) r.put(j, to_bits<T>(sum[k][j]));
+      store_piece<T>(static_cast<typename Elem<T>::type*>(a.dgain), at[k], r);
+    }
+    return;
+  }
+  float* out = blocks == 1 ? static_cast<float*>(a.dgain) : a.partial + block * a.cols;
 #pragma unroll
   for (int k = 0; k < CH; ++k)
 #pragma unroll
@@ -490,13 +500,7 @@ __global__ __launch_bounds__(kThreads) void k_rows8_dequantize(const int8_t* __r
   store_values(x + row * ldx + c, n, out);
 }
 
-// A row that stays in registers has a whole piece and at most so many of them.
-constexpr int64_t kMostPieces = 4096, kMostCols = 16384;
-
 int64_t pieces_of(int64_t cols, int type) { return ceil_div(cols, type == EMB_TYPE_FP32 ? 4 : 8); }
-bool in_registers(int64_t cols, int type) {
-  return cols >= (type == EMB_TYPE_FP32 ? 4 : 8) && cols <= kMostCols && pieces_of(cols, type) <= kMostPieces;
-}
 
 // Calls f<TEAM, CH> for a row of so many pieces; FEW: there are so few rows that each may have a CU to itself.
 template <class F>
@@ -582,17 +586,22 @@ hipError_t backward_rows_as(const NormBackward& a, bool gain_wide, int64_t slabs
 
 }  // namespace
 
+// A row that stays in registers has a whole piece and at most 4096 of them, and 16384 columns.
+bool norm_in_registers(int64_t cols, int type) { return cols >= (type == EMB_TYPE_FP32 ? 4 : 8) && cols <= 16384; }
+
 // Workgroups that share the rows, each with a part of the gain's gradient: two to a CU, but no more than have two rows a
-// team, and none with more than kNormSlabRows a team.
+// team, and none with more than kNormSlabRows a team.  Up to four rows a team are one workgroup's, which needs no join
+// (a launch of 3 us).
 int64_t norm_slabs(int64_t rows, int64_t cols, int type) {
-  if (!in_registers(cols, type)) return ceil_div(rows, kNormSlabRows);
+  if (!norm_in_registers(cols, type)) return ceil_div(rows, kNormSlabRows);
   const int64_t teams = pieces_of(cols, type) <= 256 ? 4 : 1;
+  if (rows && rows <= 4 * teams) return 1;
   const int64_t most = ceil_div(rows, 2 * teams), least = ceil_div(rows, kNormSlabRows * teams);
   return most < 512 ? most : least > 512 ? least : 512;
 }
 
 hipError_t launch_norm(const NormForward& a, int type, bool gain_wide, hipStream_t s) {
-  if (in_registers(a.cols, type)) {
+  if (norm_in_registers(a.cols, type)) {
     if (type == EMB_TYPE_FP32) return norm_rows_as<EMB_TYPE_FP32>(a, true, s);
     if (type == EMB_TYPE_BF16) return norm_rows_as<EMB_TYPE_BF16>(a, gain_wide, s);
     return norm_rows_as<EMB_TYPE_FP16>(a, gain_wide, s);
@@ -606,7 +615,7 @@ hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide,
   const int64_t slabs = norm_slabs(a.rows, a.cols, type);
   hipError_t e = hipSuccess;
   if (a.rows) {
-    if (in_registers(a.cols, type))
+    if (norm_in_registers(a.cols, type))
       e = type == EMB_TYPE_FP32   ? backward_rows_as<EMB_TYPE_FP32>(a, true, slabs, s)
           : type == EMB_TYPE_BF16 ? backward_rows_as<EMB_TYPE_BF16>(a, gain_wide, slabs, s)
                                   : backward_rows_as<EMB_TYPE_FP16>(a, gain_wide, slabs, s);
@@ -617,7 +626,8 @@ hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide,
     else
       e = gain_wide ? backward_as<EMB_TYPE_FP16, EMB_TYPE_FP32>(a, slabs, s) : backward_as<EMB_TYPE_FP16, EMB_TYPE_FP16>(a, slabs, s);
   }
-  return e == hipSuccess && a.dgain ? join(a, slabs, gain_wide ? EMB_TYPE_FP32 : type, s) : e;
+  const bool joined = slabs == 1 && norm_in_registers(a.cols, type);
+  return e == hipSuccess && a.dgain && !joined ? join(a, slabs, gain_wide ? EMB_TYPE_FP32 : type, s) : e;
 }
 
 hipError_t launch_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_t ldc, const float* scales, void* x,

@@ -143,6 +143,36 @@ bool grads_ok(const emb_clip* h, const void* const* grads) {
   return true;
 }
 
+// Whether no two gradients share memory, nor one with `other`.
+bool apart(const emb_clip* h, const void* const* grads, const void* other, size_t bytes) {
+  try {
+    std::vector<std::pair<uintptr_t, uintptr_t>> places;   // begin, end
+    places.reserve(h->sizes.size() + 1);
+    const auto add = [&](const void* p, uintptr_t n) { places.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + n); };
+    for (size_t t = 0; t < h->sizes.size(); ++t)
+      if (h->sizes[t] && grads[t]) add(grads[t], (uintptr_t)h->sizes[t] * type_bytes(h->types[t]));
+    add(other, bytes);
+    std::sort(places.begin(), places.end());
+    for (size_t i = 1; i < places.size(); ++i)
+      if (places[i].first < places[i - 1].second) return false;
+    return true;
+  } catch (const std::bad_alloc&) {
+    return false;
+  }
+}
+
+// The checks of a call that takes a norm, and the parts' sums of squares into the workspace.
+int squares(const emb_clip* h, const void* const* grads, double max_norm, float* result, void* workspace, size_t workspace_bytes,
+            void* stream) {
+  if (!h || !grads || !(max_norm > 0.0) || !result || reinterpret_cast<uintptr_t>(result) % 4 || !grads_ok(h, grads)) return EMB_EINVAL;
+  const size_t need = clip_workspace(h->part0.back());
+  if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
+  if (workspace_bytes < need) return EMB_ENOMEM;
+  return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
+    return launch_clip_squares(h->dev, ptr, first, part0, some, static_cast<double*>(workspace), S(stream));
+  }));
+}
+
 }  // namespace
 
 extern "C" {
@@ -172,7 +202,8 @@ int emb_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_
 
 int emb_rmsnorm_backward_workspace(int32_t type, int64_t rows, int64_t cols, size_t* bytes) {
   if (!bytes || !type_ok(type) || !norm_dims_ok(rows, cols)) return EMB_EINVAL;
-  *bytes = align_up((size_t)norm_slabs(rows, cols, type) * (size_t)cols * 4);
+  const int64_t slabs = norm_slabs(rows, cols, type);
+  *bytes = slabs > 1 || !norm_in_registers(cols, type) ? align_up((size_t)slabs * (size_t)cols * 4) : 0;
   return EMB_OK;
 }
 
@@ -332,39 +363,26 @@ int emb_clip_destroy(emb_clip_t h) {
 
 int emb_clip_norm(emb_clip_t h, const void* const* grads, double max_norm, float* result, void* workspace, size_t workspace_bytes,
                   void* stream) {
-  if (!h || !grads || !(max_norm > 0.0) || !result || reinterpret_cast<uintptr_t>(result) % 4 || !grads_ok(h, grads)) return EMB_EINVAL;
-  const int64_t parts = h->part0.back();
-  const size_t need = clip_workspace(parts);
-  if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
-  if (workspace_bytes < need) return EMB_ENOMEM;
-  double* partial = static_cast<double*>(workspace);
-  const hipError_t e = over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
-    return launch_clip_squares(h->dev, ptr, first, part0, some, partial, S(stream));
-  });
-  if (e != hipSuccess) return EMB_EHIP;
-  return status(launch_clip_join(partial, parts, max_norm, result, S(stream)));
+  const int st = squares(h, grads, max_norm, result, workspace, workspace_bytes, stream);
+  return st != EMB_OK ? st : status(launch_clip_join(static_cast<const double*>(workspace), h->part0.back(), max_norm, result, S(stream)));
 }
 
 int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* stream) {
-  if (!h || !grads || !factor || reinterpret_cast<uintptr_t>(factor) % 4 || !grads_ok(h, grads)) return EMB_EINVAL;
-  try {
-    std::vector<std::pair<uintptr_t, uintptr_t>> places;   // begin, end
-    places.reserve(h->sizes.size() + 1);
-    for (size_t t = 0; t < h->sizes.size(); ++t)
-      if (h->sizes[t] && grads[t]) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(grads[t]);
-        places.emplace_back(at, at + (uintptr_t)h->sizes[t] * type_bytes(h->types[t]));
-      }
-    const uintptr_t f = reinterpret_cast<uintptr_t>(factor);
-    places.emplace_back(f, f + 4);
-    std::sort(places.begin(), places.end());
-    for (size_t i = 1; i < places.size(); ++i)
-      if (places[i].first < places[i - 1].second) return EMB_EINVAL;
-  } catch (const std::bad_alloc&) {
-    return EMB_EINVAL;
-  }
+  if (!h || !grads || !factor || reinterpret_cast<uintptr_t>(factor) % 4 || !grads_ok(h, grads) || !apart(h, grads, factor, 4)) return EMB_EINVAL;
   return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
     return launch_clip_scale(h->dev, ptr, first, part0, some, factor, S(stream));
+  }));
+}
+
+int emb_clip_apply(emb_clip_t h, void* const* grads, double max_norm, float* result, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  if (!h || !grads || !result || !grads_ok(h, grads) || !apart(h, grads, result, 8)) return EMB_EINVAL;
+  const int64_t parts = h->part0.back();
+  if (!parts) return emb_clip_norm(h, grads, max_norm, result, workspace, workspace_bytes, stream);
+  const int st = squares(h, grads, max_norm, result, workspace, workspace_bytes, stream);
+  if (st != EMB_OK) return st;
+  return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
+    return launch_clip_join_scale(h->dev, ptr, first, part0, some, static_cast<const double*>(workspace), parts, max_norm, result, S(stream));
   }));
 }
 

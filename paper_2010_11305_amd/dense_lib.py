@@ -101,6 +101,7 @@ def load():
         "emb_clip_destroy": [P],
         "emb_clip_norm": [P, P, f64, P, P, size, P],
         "emb_clip_scale": [P, P, P, P],
+        "emb_clip_apply": [P, P, f64, P, P, size, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -126,6 +127,27 @@ def call(name: str, device, *args):
     else:
         with torch.cuda.device(index):
             status = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        raise emb_cache.EmbCacheError(status, name)
+
+
+def call_in(name: str, device, need: int, *args):
+    """call() for a function whose last arguments before the stream are a workspace and its size: `need` bytes of torch's
+    allocator, given back as soon as the call has enqueued its kernels (the stream orders whoever gets them next, also in
+    a captured graph).  Without a tensor around them they cost a third of one."""
+    if not need:
+        return call(name, device, *args, None, 0)
+    index = device.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return call_in(name, device, need, *args)
+    f = getattr(_lib or load(), name)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    ws = torch._C._cuda_cudaCachingAllocator_raw_alloc(need, stream)
+    try:
+        status = f(*args, ws, need, stream)
+    finally:
+        torch._C._cuda_cudaCachingAllocator_raw_delete(ws)
     if status:
         raise emb_cache.EmbCacheError(status, name)
 
@@ -171,7 +193,7 @@ def type_of(dtype) -> int:
 def result(out, rows, cols, dtype, device):
     """(out, pointer, type, row stride) of a result [rows, cols], new where none is given."""
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=device)
+        out = torch.empty(rows, cols, dtype=dtype, device=device)
         return out, out.data_ptr(), type_of(dtype), max(cols, 1)
     p, t, r, c, ld = matrix(out, "out")
     if r != rows or c != cols or out.device != device:

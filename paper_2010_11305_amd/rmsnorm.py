@@ -110,12 +110,13 @@ def norm8(x, gain=None, residual=None, eps=1e-6, sum_out=None):
     """(Rows8, h): norm, with y in 8 bits and a scale a row."""
     head, sum_part, h, changed = _inputs(x, gain, residual, sum_out)
     rows, cols = head[2:4]
-    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
-    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    q = Rows8.__new__(Rows8)   # made here, so there is nothing to check
+    q.codes = codes = torch.empty(rows, cols, dtype=torch.int8, device=x.device)
+    q.scales = scales = torch.empty(rows, dtype=torch.float32, device=x.device)
     lib.call("emb_rmsnorm_forward8", x.device, *head, eps, *sum_part, codes.data_ptr(), cols, scales.data_ptr())
     if changed:
         lib.written(changed)
-    return Rows8(codes, scales), h
+    return q, h
 
 
 def backward(dy, h, inverse, gain=None, dh=None, out=None):
@@ -137,14 +138,12 @@ def backward(dy, h, inverse, gain=None, dh=None, out=None):
     dx, xp, xt, x_ld = lib.result(out, rows, cols, dy.dtype, dev)
     if xt != t:
         raise ValueError("out must have the type of dy")
-    dgain = ws = None
-    need = 0
+    dgain, need = None, 0
     if gain is not None:
         dgain = torch.empty(cols, dtype=gain.dtype, device=dev)
         need = lib.query("emb_rmsnorm_backward_workspace", t, rows, cols)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    lib.call("emb_rmsnorm_backward", dev, p, t, rows, cols, ld, hp, h_ld, inverse.data_ptr(), g, gt, s, s_ld, xp, x_ld,
-             dgain.data_ptr() if gain is not None else None, ws.data_ptr() if need else None, need)
+    lib.call_in("emb_rmsnorm_backward", dev, need, p, t, rows, cols, ld, hp, h_ld, inverse.data_ptr(), g, gt, s, s_ld, xp, x_ld,
+                dgain.data_ptr() if gain is not None else None)
     if out is not None:
         lib.written([out])
     return dx, dgain

@@ -109,10 +109,8 @@ def linear(x, w: W4Matrix, bias=None, relu: bool = False, dtype=None, out=None):
         b = bias.data_ptr()
     given = out is not None
     out, yp, yt, y_ld = lib.result(out, m, n, dtype, dev)
-    need = lib.query("emb_w4_linear_workspace", t, m, n, k, w.group)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    lib.call("emb_w4_linear", dev, p, t, scales, m, k, ld, w.data.data_ptr(), n, w.group, b, bool(relu), yp, yt, y_ld,
-             ws.data_ptr() if need else None, need)
+    lib.call_in("emb_w4_linear", dev, lib.query("emb_w4_linear_workspace", t, m, n, k, w.group), p, t, scales, m, k, ld,
+                w.data.data_ptr(), n, w.group, b, bool(relu), yp, yt, y_ld)
     if given:
         lib.written([out])
     return out

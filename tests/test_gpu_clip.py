@@ -49,6 +49,10 @@ def test_norm_and_clipping(torch, name, dtypes):
         assert norm2 == norm and factor2 == factor
         for a, g in zip(t, grads):
             assert torch.equal(a, (g.float() * factor).to(g.dtype))
+        t = [g.clone() for g in grads]
+        c.scale_(t, factor)
+        for a, g in zip(t, grads):
+            assert torch.equal(a, (g.float() * factor).to(g.dtype))
 
 
 def test_missing_gradients_and_views(torch):
@@ -152,9 +156,14 @@ def test_refusals(torch):
     same = torch.ones(50, device="cuda")
     shared = [same[:40], same[39:47]]
     assert abs(float(c.norm(shared)[0]) - 48**0.5) < 1e-6     # read only
-    with pytest.raises(Exception, match="emb_clip_scale"):
+    with pytest.raises(Exception, match="emb_clip_apply"):
         c.clip_(shared)
+    with pytest.raises(Exception, match="emb_clip_scale"):
+        c.scale_(shared, torch.zeros(1, device="cuda"))
     assert (same == 1).all()
+    for bad in (torch.ones(1), torch.ones(2, device="cuda"), torch.ones(1, device="cuda").half()):
+        with pytest.raises(ValueError):
+            c.scale_(g, bad)
 
 
 def test_written_tensors_count_as_changed(torch):

@@ -27,7 +27,7 @@ def L():
 def test_every_declared_symbol_is_exported(L):
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "emb_dense.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(emb_(?:rmsnorm|rows8|w4|clip)_\w+)\s*\(", text)))
-    assert len(names) == 17
+    assert len(names) == 18
     for n in names:
         assert ctypes.cast(getattr(L, n), ctypes.c_void_p).value
 
@@ -79,12 +79,14 @@ def test_norm_backward_refusals(L):
         assert L.emb_rmsnorm_backward_workspace(type, rows, cols, ctypes.byref(n)) == 0
         # at most 4 teams of 256 rows share a part, and there are no more parts than rows
         assert n.value % 256 == 0 and n.value >= rows // 1024 * cols * 4 and n.value <= 4 * rows * cols + 255
+    for type, rows, cols, want in ((1, 16, 2048, 0), (1, 17, 2048, 3 * 2048 * 4), (1, 4, 8192, 0), (0, 1, 5, 0), (0, 2, 3, 256), (1, 1, 20000, 80128)):
+        assert L.emb_rmsnorm_backward_workspace(type, rows, cols, ctypes.byref(n)) == 0 and n.value == want
     assert L.emb_rmsnorm_backward_workspace(1, 4, 40, None) == EINVAL
     assert L.emb_rmsnorm_backward_workspace(1, 4, 0, ctypes.byref(n)) == EINVAL and L.emb_rmsnorm_backward_workspace(3, 4, 40, ctypes.byref(n)) == EINVAL
-    assert L.emb_rmsnorm_backward_workspace(1, 4, 40, ctypes.byref(n)) == 0
+    assert L.emb_rmsnorm_backward_workspace(1, 40, 40, ctypes.byref(n)) == 0 and n.value
 
     def call(**kw):
-        a = dict(dy=FAKE, type=1, rows=4, cols=40, lddy=40, h=FAR, ldh=40, inv=2 * FAR, g=3 * FAR, gt=0, ds=4 * FAR, ldds=40, dx=5 * FAR, lddx=40,
+        a = dict(dy=FAKE, type=1, rows=40, cols=40, lddy=40, h=FAR, ldh=40, inv=2 * FAR, g=3 * FAR, gt=0, ds=4 * FAR, ldds=40, dx=5 * FAR, lddx=40,
                  dg=6 * FAR, ws=7 * FAR, wsb=n.value)
         a.update(kw)
         return L.emb_rmsnorm_backward(*a.values(), None)
@@ -172,6 +174,7 @@ def test_clip_refusals(L):
         assert L.emb_clip_create(ctypes.byref(c), state, nbytes, None, ctypes.byref(h)) == want and not h.value
     assert L.emb_clip_norm(None, FAKE, 1.0, FAKE, FAKE, 1 << 20, None) == EINVAL
     assert L.emb_clip_scale(None, FAKE, FAKE, None) == EINVAL
+    assert L.emb_clip_apply(None, FAKE, 1.0, FAKE, FAKE, 1 << 20, None) == EINVAL
     assert L.emb_clip_destroy(None) == 0
 
 
