@@ -200,7 +200,7 @@ constexpr int kClipTensors = 480;   // tensors whose pointers one launch carries
 struct ClipTensor {
   int64_t size;
   int32_t type;
-  int32_t pad;
+  uint32_t parts;   // workgroups that share it
 };
 
 struct ClipPointers {
@@ -209,8 +209,7 @@ struct ClipPointers {
 
 struct ClipDev {
   const ClipTensor* tensors;
-  const AdamPart* parts;
-  int64_t chunk;   // elements of a part
+  const AdamPart* parts;   // chunk: which of a tensor's parts
 };
 
 // Squares of parts [part0, part0 + parts) of tensors from `first` on, into partial[part].

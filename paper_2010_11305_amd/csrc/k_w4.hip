@@ -40,6 +40,24 @@ __device__ __forceinline__ int columns(const W4& q, const Place& p, int i, int64
 // Codes (0 .. 15 each) of 8 columns to a dword of a tile, and back.
 __device__ __forceinline__ int shift_of(int j) { return j < 4 ? 8 * j : 8 * (j - 4) + 4; }
 
+// 8 plain codes, column j in nibble j, to a dword of a tile, and back: columns 0 .. 3 in the even nibbles, 4 .. 7 in the odd.
+__device__ __forceinline__ uint32_t spread(uint32_t x) {
+  x = (x | x << 8) & 0x00FF00FFu;
+  return (x | x << 4) & 0x0F0F0F0Fu;
+}
+__device__ __forceinline__ uint32_t tiled(uint32_t plain) { return spread(plain & 0xFFFFu) | spread(plain >> 16) << 4; }
+__device__ __forceinline__ uint32_t gathered(uint32_t x) {
+  x &= 0x0F0F0F0Fu;
+  x = (x | x >> 4) & 0x00FF00FFu;
+  return (x | x >> 8) & 0xFFFFu;
+}
+__device__ __forceinline__ uint32_t plain(uint32_t tile) { return gathered(tile) | gathered(tile >> 4) << 16; }
+
+// Four bytes at any address.
+struct __attribute__((packed, aligned(1))) Bytes4 {
+  uint32_t w;
+};
+
 template <int TYPE, int G>
 __global__ __launch_bounds__(kThreads) void k_w4_quantize(const typename Elem<TYPE>::type* __restrict__ x, int64_t ld, W4 q,
                                                           uint8_t* __restrict__ out, int64_t first) {
@@ -136,10 +154,13 @@ __global__ __launch_bounds__(kThreads) void k_w4_pack(const uint8_t* __restrict_
   for (int i = 0; i < 4; ++i) {
     int64_t c;
     const int n = columns(q, p, i, &c);
+    const uint8_t* from = codes + p.row * pitch + c / 2;
     word[i] = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) word[i] |= (uint32_t)(codes[p.row * pitch + (c + j) / 2] >> (4 * (j % 2)) & 15) << shift_of(j);
+    if (n == 8) {
+      word[i] = tiled(reinterpret_cast<const Bytes4*>(from)->w);
+    } else {
+      for (int j = 0; j < n; ++j) word[i] |= (uint32_t)(from[j / 2] >> (4 * (j % 2)) & 15) << shift_of(j);
+    }
   }
   reinterpret_cast<uint4*>(out + q.tile(p.rt, p.kt))[p.lane] = make_uint4(word[0], word[1], word[2], word[3]);
   const int per = kTileCols / q.group;
@@ -162,11 +183,13 @@ __global__ __launch_bounds__(kThreads) void k_w4_unpack(W4 q, uint8_t* __restric
   for (int i = 0; i < 4; ++i) {
     int64_t c;
     const int n = columns(q, p, i, &c);
-#pragma unroll
-    for (int j = 0; j < 8; j += 2)
-      if (j < n)
-        codes[p.row * pitch + (c + j) / 2] =
-            (uint8_t)((word[i] >> shift_of(j) & 15u) | (j + 1 < n ? (word[i] >> shift_of(j + 1) & 15u) << 4 : 0u));
+    uint8_t* to = codes + p.row * pitch + c / 2;
+    if (n == 8) {
+      reinterpret_cast<Bytes4*>(to)->w = plain(word[i]);
+    } else {
+      for (int j = 0; j < n; j += 2)
+        to[j / 2] = (uint8_t)((word[i] >> shift_of(j) & 15u) | (j + 1 < n ? (word[i] >> shift_of(j + 1) & 15u) << 4 : 0u));
+    }
   }
   const int per = kTileCols / q.group;
   const int64_t g = p.kt * per + p.b;

@@ -86,11 +86,10 @@ namespace {
 struct ClipPlan {
   std::vector<ClipTensor> tensors;
   std::vector<int64_t> part0;
-  int64_t chunk = 0;
   size_t o_tensors, o_parts, bytes;
 };
 
-// Elements of a part: few enough that small models fill the device, many enough that the parts of a large one are
+// Elements for a workgroup: few enough that small models fill the device, many enough that the parts of a large one are
 // soon joined.
 constexpr int64_t kClipLeast = 2048, kClipParts = 2048;
 
@@ -105,12 +104,13 @@ int plan_clip(const emb_clip_config* c, ClipPlan* p) {
     total += n;
     if (total > ((int64_t)1 << 40)) return EMB_EINVAL;
   }
-  p->chunk = kClipLeast;
-  while (total / p->chunk > kClipParts) p->chunk *= 2;
+  int64_t chunk = kClipLeast;
+  while (total / chunk > kClipParts) chunk *= 2;
   int64_t parts = 0;
-  for (const ClipTensor& t : p->tensors) {
+  for (ClipTensor& t : p->tensors) {
     p->part0.push_back(parts);
-    parts += ceil_div(t.size, p->chunk);
+    t.parts = (uint32_t)ceil_div(t.size, chunk);
+    parts += t.parts;
   }
   p->part0.push_back(parts);
   p->o_tensors = 0;
@@ -338,7 +338,7 @@ int emb_clip_create(const emb_clip_config* cfg, void* state, size_t state_bytes,
     }
     h->part0 = p.part0;
     uint8_t* b = static_cast<uint8_t*>(state);
-    h->dev = {reinterpret_cast<const ClipTensor*>(b + p.o_tensors), reinterpret_cast<const AdamPart*>(b + p.o_parts), p.chunk};
+    h->dev = {reinterpret_cast<const ClipTensor*>(b + p.o_tensors), reinterpret_cast<const AdamPart*>(b + p.o_parts)};
     hipError_t e = hipMemcpyAsync(b + p.o_tensors, p.tensors.data(), sizeof(ClipTensor) * p.tensors.size(), hipMemcpyHostToDevice, S(stream));
     if (e == hipSuccess && !parts.empty())
       e = hipMemcpyAsync(b + p.o_parts, parts.data(), sizeof(AdamPart) * parts.size(), hipMemcpyHostToDevice, S(stream));
