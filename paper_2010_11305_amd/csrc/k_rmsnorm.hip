@@ -3,6 +3,12 @@
 // Rows of at most 4096 pieces of 16 bytes (and 16384 columns) stay in the registers of a team of threads, which reads and
 // writes every value once; wider ones take a workgroup a row that goes over it as often as it has to, a thread
 // always over the same 8 columns at a time, so that what it wrote in one pass it reads in the next.
+//
+// Memory bounds them.  16384 x 12800 BF16 with a residual (1.68 GB each way): forward 277 us (6.1 TB/s), gradients 324 (5.2) and
+// 7.6 to join 512 parts of the gain's; in passes over memory the same took 348 and 706.  4096 x 8192 to 8 bits, with a
+// residual, 47.7 us (4.9 TB/s), the codes to BF16 16.8 (6.0).  What little there is takes the launch and two or three trips to
+// memory: 2048 x 416 FP32 3.7, 5.2 and 2.5 us, one row of 12800 to 8 bits 4.7.
+// Squares are summed in FP64, which costs nothing there: no row of FP32 overflows or vanishes.
 #include "dense_device.h"
 
 namespace embd {

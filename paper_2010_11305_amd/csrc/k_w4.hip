@@ -2,6 +2,9 @@
 //
 // A wave takes a tile of 16 rows x 128 columns; lane 16 b + r holds columns 32 i + 8 b + (0 .. 7) of row r for i = 0 .. 3,
 // so a group of 32 columns is four lanes' values of one i, one of 64 or 128 of two or four.
+//
+// 8192 x 12800, groups of 128 (BF16 210 MB, the matrix 55.7 MB): quantisation 78 us (3.4 TB/s; an IEEE division a value, as the
+// tables' rows have it), expansion 45 us (5.9 TB/s), plain form to tiles and back 36 and 37 us, 3 TB/s.
 #include "dense_device.h"
 
 namespace embd {

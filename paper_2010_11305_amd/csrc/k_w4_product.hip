@@ -4,6 +4,15 @@
 // instruction's first operand as they are, small whole numbers that every type here holds exactly; the sums of x come from
 // the same instruction with ones in their place, in the registers where the sums of products lie.  FP32 rows go
 // in as three BF16 parts that add up to them exactly.
+//
+// Few rows (k_w4_few) are bound by memory and by what every launch costs: 1 row, 4096 x 12800, groups of 128, 7.5 us a
+// call for 27.9 MB (3.7 TB/s), of which 3.3 us are left without the loop over the columns; 8-bit rows against 8192 x 8192
+// 8.2 us for 35.7 MB (4.4 TB/s).  Code runs once or twice in such a call, and its way from memory counts as much as the data's: with the
+// loop unrolled over 7 tiles, whose loads were all under way at once, the same took 10.5 and 12.7 us.  So loops stay short,
+// and what is rare goes value by value.
+// Up to 64 rows (k_w4_more): 64 rows, 8192 x 12800, 31.5 us with groups of 32 and 29 with groups of 128 (430 and 460 TFLOP/s), k_w4_rows'
+// 4 among them.  200 vector operations a wave and tile (128 of them scale sums), 40 matrix instructions and 420 MB of x out of the L2
+// take about as long each: without the loads of x 28 and 21 us, without those of w 27 and 25, without matrix instructions 32 and 20.
 #include "dense_device.h"
 
 namespace embd {
@@ -41,8 +50,8 @@ __device__ __forceinline__ u32x4 code_values(uint32_t w) {
   return v;
 }
 
-// 16 rows x 128 columns of x as the second operand: lane 16 b + r holds columns 32 i + 8 b + (0 .. 7) of row r.
-// kSets registers sets of 16 bytes: for i = 0 .. 3 of each part of FP32 rows, or i = 0, 1 and 2, 3 of 8-bit rows.
+// 16 rows x 128 columns of x as the second operand: lane 16 b + r holds columns 32 i + 8 b + (0 .. 7) of row r, in kSets sets
+// of 16 bytes: one for each i = 0 .. 3 (and each part of FP32 rows), or for i = 0, 1 and i = 2, 3 of 8-bit rows.
 template <int T>
 struct Tile {
   static constexpr int kParts = T == EMB_TYPE_FP32 ? 3 : 1;
@@ -267,7 +276,8 @@ __device__ __forceinline__ void finish(const W4Linear& a, int64_t row, int64_t n
 // A workgroup computes 16 outputs of up to 16 rows; its waves (up to 16) share the column tiles.  All of the rows are in
 // LDS, in the order of the operand; FP32 ones as they are (RAW) where their three parts would not fit.
 constexpr int kFewWaves = 16;
-constexpr int kFewLds = 65536, kFewLdsRaw = 131072;
+constexpr int kFewLds = 65536;       // two workgroups to a CU
+constexpr int kFewLdsRaw = 131072;   // one
 template <int T, int G, bool RAW>
 __global__ __launch_bounds__(64 * kFewWaves) void k_w4_few(W4Linear a, W4 w, int64_t first) {
   constexpr int kPer = kTileCols / G, kSets = Tile<T>::kSets;
@@ -356,8 +366,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_w4_few(W4Linear a, W4 w, int
 
 // ---- more rows -----------------------------------------------------------------------------------
 // x first goes through the workspace: tiles of 16 rows x 128 columns in the order of the operand, zeros past the last
-// column, and the sums of their groups.  Every workgroup reads all of them, whole lines at a time; rows of x lie a power
-// of two apart often enough, and then all are in one channel of the L2 (48 x 4096 x 8192 in 8 bits with x read as it lies: 26 us).
+// column, and the sums of their groups.  Every workgroup reads all of them, whole lines at a time.  Read as they lie, rows a
+// power of two apart are in one channel of the L2 (48 x 4096 x 8192 in 8 bits: 26 us, so 12.5); tiles in LDS that 128 outputs
+// share make all waves wait for each other, and shares of the columns another launch (17 us).
 struct Prepared {
   u32x4* x;       // [column tile][tile of 16 rows][set][lane]
   float* sums;    // [column tile][tile of 16 rows][lane]: of group b and row r at 16 b + r
