@@ -281,8 +281,9 @@ int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint
  *   type      of x: a full-precision type, or EMB_TYPE_INT8 with `scales` [m], the rows' scales (NULL otherwise)
  *   bias      [n] FP32, or NULL
  *   y_type    a full-precision type
- * A group's products are summed over its codes and its biases apart, scale * sum(q x) + bias * sum(x): exact products,
- * sums in FP32 (of 8-bit rows exact integers within a group), one rounding to y_type.  A row of x that is not finite, or
+ * A group's products are summed over its codes and its biases apart, scale * sum(q x) + bias * sum(x): exact products (of
+ * FP32 rows, what is below 2^-133 of a value is left out), sums in FP32 (of 8-bit rows exact integers within a group),
+ * one rounding to y_type.  A row of x that is not finite, or
  * whose sums with codes of up to 15 overflow FP32, gives values that are not finite.  The order of the sums is a function of type, m, n, k
  * and group.  y must share no element with x.
  * workspace: emb_w4_linear_workspace bytes, 256-byte aligned, or NULL when that is 0.  Enqueue-only. */

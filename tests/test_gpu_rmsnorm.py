@@ -247,6 +247,11 @@ def test_in_place(torch, cols):
         t = {"x": x.clone(), "r": r.clone(), None: None}
         got = rmsnorm.norm(t["x"], gain, residual=t["r"], out=t[over_y], sum_out=t[over_h])
         assert torch.equal(got[0], y) and torch.equal(got[1], h)
+    q, _ = rmsnorm.norm8(x, gain, residual=r)
+    for over in (0, 1):
+        t = [x.clone(), r.clone()]
+        got, sum_out = rmsnorm.norm8(t[0], gain, residual=t[1], sum_out=t[over])
+        assert sum_out is t[over] and torch.equal(sum_out, h) and torch.equal(got.codes, q.codes) and torch.equal(got.scales, q.scales)
     dx, dgain = rmsnorm.backward(dy, h, inverse, gain, dh=dh)
     for over in range(3):
         t = [v.clone() for v in (dy, h, dh)]

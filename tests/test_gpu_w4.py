@@ -216,6 +216,22 @@ def test_strides_and_odd_addresses(torch, dtype):
     assert torch.equal(wide[:, 3:203], w4.quantize(x, 32).dequantize()) and (wide[:, :3] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_subnormal_rows(torch, dtype):
+    """One column, a code of 1, scale 1 and bias 0, by both routes: values below the normal numbers arrive as they are."""
+    from paper_2010_11305_amd import w4
+
+    least = {"bf16": -133, "fp16": -24}[dtype]
+    for m, n, k in ((16, 1, 1), (16, 20, 8200)):
+        codes, scales = torch.zeros((n, -(-k // 2)), dtype=torch.uint8, device="cuda"), torch.ones((n, -(-k // 32)), device="cuda").half()
+        codes[:, 0] = 1
+        w = w4.from_codes(codes, scales, torch.zeros_like(scales), k, 32)
+        x = torch.zeros((m, k), dtype=DTYPES[dtype], device="cuda")
+        x[:, 0] = torch.tensor([(1 + e % 7) * 2.0 ** (least + e // 2) for e in range(m)], dtype=torch.float64).to(x.dtype)
+        assert (x[:, 0] != 0).all()
+        assert torch.equal(w4.linear(x, w, dtype=torch.float32), x[:, :1].float().expand(m, n))
+
+
 def test_rows_that_are_not_finite(torch):
     """They spoil their own outputs alone, also where the activation follows; a row in 8 bits whose scale is NaN too."""
     from paper_2010_11305_amd import rmsnorm, w4
@@ -284,9 +300,11 @@ def test_graph_and_streams(torch):
     w = w4.quantize(torch.from_numpy(weight(600, 2000)).float().cuda(), 128)
     b = torch.randn(600, device="cuda")
     graphs = []
+    large = w4.quantize(torch.from_numpy(weight(4000, 2000)).float().cuda(), 64)     # of 40 rows, these go through a workspace
     for m in (1, 40):
         x = torch.randn((m, 2000), device="cuda").bfloat16()
-        step = lambda x=x: (w4.linear(x, w, bias=b, relu=True), w4.linear(rmsnorm.norm8(x)[0], w))  # noqa: E731
+        step = lambda x=x: (w4.linear(x, w, bias=b, relu=True), w4.linear(rmsnorm.norm8(x)[0], w), w4.linear(x, large),  # noqa: E731
+                            w4.linear(rmsnorm.norm8(x)[0], large))
         step()
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
@@ -302,13 +320,16 @@ def test_graph_and_streams(torch):
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
-        got = graphs[0][2]()
-    want = graphs[0][2]()
+        got = [graphs[1][2]() for _ in range(4)]
+    want = [graphs[0][2]() for _ in range(4)]      # at the same time
     torch.cuda.synchronize()
-    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    for (_, _, step, _), calls in zip(graphs, (want, got)):
+        expect = step()
+        assert all(torch.equal(a, c) for call in calls for a, c in zip(call, expect))
 
 
-LARGE = [(16, 33, 8200), (16, 8200, 8200), (17, 4000, 2200), (20, 8200, 1200), (40, 3000, 2100), (48, 8177, 700), (64, 2100, 2100), (70, 8200, 520), (7, 50, 4100),
+# the largest rows that k_w4_few holds as operands (16 x 2048 in 16 bits) and as FP32 (16 x 2048), and those past them
+LARGE = [(16, 40, 2048), (16, 40, 2049), (5, 40, 6500), (16, 20, 4096), (16, 20, 4097), (16, 33, 8200), (16, 8200, 8200), (17, 4000, 2200), (20, 8200, 1200), (40, 3000, 2100), (48, 8177, 700), (64, 2100, 2100), (70, 8200, 520), (7, 50, 4100),
          (200, 1700, 1000)]
 
 
