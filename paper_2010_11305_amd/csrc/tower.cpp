@@ -143,15 +143,30 @@ bool grads_ok(const emb_clip* h, const void* const* grads) {
   return true;
 }
 
-// Whether no two gradients share memory, nor one with `other`.
+// Whether no two gradients share memory, nor one with `other`.  Gradients mostly lie one behind the other already.
 bool apart(const emb_clip* h, const void* const* grads, const void* other, size_t bytes) {
+  const uintptr_t o = reinterpret_cast<uintptr_t>(other);
+  const auto place = [&](size_t t) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(grads[t]);
+    return std::pair<uintptr_t, uintptr_t>(at, at + (uintptr_t)h->sizes[t] * type_bytes(h->types[t]));
+  };
+  uintptr_t end = 0;
+  bool rising = true;
+  size_t there = 0;
+  for (size_t t = 0; t < h->sizes.size(); ++t) {
+    if (!h->sizes[t] || !grads[t]) continue;
+    const auto p = place(t);
+    if (p.first < o + bytes && o < p.second) return false;
+    rising = rising && p.first >= end;
+    end = p.second;
+    ++there;
+  }
+  if (rising) return true;
   try {
-    std::vector<std::pair<uintptr_t, uintptr_t>> places;   // begin, end
-    places.reserve(h->sizes.size() + 1);
-    const auto add = [&](const void* p, uintptr_t n) { places.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + n); };
+    std::vector<std::pair<uintptr_t, uintptr_t>> places;
+    places.reserve(there);
     for (size_t t = 0; t < h->sizes.size(); ++t)
-      if (h->sizes[t] && grads[t]) add(grads[t], (uintptr_t)h->sizes[t] * type_bytes(h->types[t]));
-    add(other, bytes);
+      if (h->sizes[t] && grads[t]) places.push_back(place(t));
     std::sort(places.begin(), places.end());
     for (size_t i = 1; i < places.size(); ++i)
       if (places[i].first < places[i - 1].second) return false;
