@@ -246,26 +246,41 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_row(NormForward a, bool g
   }
 }
 
-// The gradients, rows in the registers of a team: a workgroup takes every blocks-th row (or group of rows, a team each),
-// keeps its columns' part of the gain's gradient in registers and leaves it in `partial` (a single one: in `dgain`).
-template <int T, int TEAM, int CH>
-__global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a, bool gain_wide, int64_t first, int64_t blocks) {
-  constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM;
-  __shared__ float sums[TEAM / 64];
-  __shared__ float meet[kTeams > 1 ? kTeams - 1 : 1][kTeams > 1 ? CH * N * TEAM : 1];
-  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  const int64_t block = first + blockIdx.x;
-  Piece at[CH];
-  float g[CH][N], sum[CH][N];
+template <int T>
+__device__ __forceinline__ void store_gain(const NormBackward& a, bool gain_wide, const Piece& at, const float (&v)[kPiece<T>]) {
+  constexpr int N = kPiece<T>;
+  if (T == EMB_TYPE_FP32 || gain_wide) {
+#pragma unroll
+    for (int q = 0; q < N; q += 4) {
+      Raw<EMB_TYPE_FP32, 4> r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[j] = __float_as_uint(v[q + j]);
+      store_piece<EMB_TYPE_FP32>(static_cast<float*>(a.dgain) + q, at, r);
+    }
+  } else if constexpr (T != EMB_TYPE_FP32) {
+    Raw<T, N> r = {};
+#pragma unroll
+    for (int j = 0; j < N; ++j) r.put(j, to_bits<T>(v[j]));
+    store_piece<T>(static_cast<uint16_t*>(a.dgain), at, r);
+  }
+}
+
+// Rows first, first + step, .. in the registers of a team.  SUMS: their part of the gain's gradient goes to `sum`.
+template <int T, int TEAM, int CH, bool SUMS>
+__device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_wide, int64_t first, int64_t step, int t, float* sums,
+                                              Piece (&at)[CH], float (&sum)[SUMS ? CH : 1][kPiece<T>]) {
+  constexpr int N = kPiece<T>;
+  float g[CH][N];
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
     at[k] = piece_of<T, TEAM, CH>(a.cols, k, t);
     gain_piece<T>(a.gain, gain_wide, at[k], g[k]);
+    if constexpr (SUMS)
 #pragma unroll
-    for (int j = 0; j < N; ++j) sum[k][j] = 0.0f;
+      for (int j = 0; j < N; ++j) sum[k][j] = 0.0f;
   }
   const float cols = (float)a.cols;
-  for (int64_t row = block * kTeams + team; row < a.rows; row += blocks * kTeams) {
+  for (int64_t row = first; row < a.rows; row += step) {
     Raw<T, N> d[CH], h[CH], s[CH] = {};
 #pragma unroll
     for (int k = 0; k < CH; ++k) d[k] = load_piece<T>(row_of<T>(a.dy, row), at[k]);
@@ -283,7 +298,7 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
       for (int j = 0; j < N; ++j) {
         const float u = h[k].get(j) * inverse, dj = d[k].get(j);
         along = fmaf(k < CH / 2 || j >= at[k].skip ? dj * g[k][j] : 0.0f, u, along);
-        sum[k][j] = fmaf(dj, u, sum[k][j]);
+        if constexpr (SUMS) sum[k][j] = fmaf(dj, u, sum[k][j]);
       }
     const float mean = block_sum<float, TEAM>(along, sums) / cols;
 #pragma unroll
@@ -295,6 +310,20 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
       store_piece<T>(row_of<T>(a.dx, row), at[k], out);
     }
   }
+}
+
+// The gradients: a workgroup takes every blocks-th row (or group of rows, a team each), keeps its columns' part of the gain's
+// gradient in registers and leaves it in `partial`.
+template <int T, int TEAM, int CH>
+__global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a, bool gain_wide, int64_t first, int64_t blocks) {
+  constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM;
+  __shared__ float sums[TEAM / 64];
+  __shared__ float meet[kTeams > 1 ? kTeams - 1 : 1][kTeams > 1 ? CH * N * TEAM : 1];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  const int64_t block = first + blockIdx.x;
+  Piece at[CH];
+  float sum[CH][N];
+  gradient_rows<T, TEAM, CH, true>(a, gain_wide, block * kTeams + team, blocks * kTeams, t, sums, at, sum);
   if (!a.dgain) return;
   if constexpr (kTeams > 1) {
     if (team) {
@@ -311,17 +340,7 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
       for (int j = 0; j < N; ++j)
         for (int o = 0; o < kTeams - 1; ++o) sum[k][j] += meet[o][(k * N + j) * TEAM + t];
   }
-  if (T != EMB_TYPE_FP32 && !gain_wide && blocks == 1) {
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      Raw<T, N> r = {};
-#pragma unroll
-      for (int j = 0; j < N; ++j) r.put(j, to_bits<T>(sum[k][j]));
-      store_piece<T>(static_cast<typename Elem<T>::type*>(a.dgain), at[k], r);
-    }
-    return;
-  }
-  float* out = blocks == 1 ? static_cast<float*>(a.dgain) : a.partial + block * a.cols;
+  float* out = a.partial + block * a.cols;
 #pragma unroll
   for (int k = 0; k < CH; ++k)
 #pragma unroll
@@ -331,6 +350,50 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
       for (int j = 0; j < 4; ++j) r.w[j] = __float_as_uint(sum[k][q + j]);
       store_piece<EMB_TYPE_FP32>(out + q, at[k], r);
     }
+}
+
+// Both gradients of few rows in one launch, without parts that a second one joins: the first `columns` workgroups each sum
+// four pieces of the gain's gradient over all rows, the others take the rows.  dy and h are read twice, the second time
+// from a cache.  Measured against k_norm_gradients and k_norm_gain_join, us in a graph: 256 x 416 in FP32 2.8 (5.4),
+// 256 x 8192 in BF16 4.7 (11.3), 1000 x 2048 in BF16 6.8 (9.4), 1000 x 1029 in FP32 8.1 (10.2); not taken beyond kOnceRows
+// and kOnceBytes: 2048 x 416 in FP32 8.6 (6.1), 1000 x 2048 in FP32 11.2 (11.1).  A dx that lies over dy or h waits for
+// the columns: two launches of the same kernel, with the same results (256 x 416 5.6, 1000 x 2048 in BF16 14.1).
+constexpr int kOncePieces = 4;
+template <int T, int TEAM, int CH>
+__global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients_once(NormBackward a, bool gain_wide, uint32_t columns) {
+  constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM, kRows = kGroup<TEAM> / kOncePieces, kWaves = kGroup<TEAM> / 64;
+  __shared__ float sums[TEAM / 64];
+  __shared__ float meet[kWaves][kOncePieces][N];
+  if (blockIdx.x >= columns) {
+    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    Piece at[CH];
+    float none[1][N];
+    gradient_rows<T, TEAM, CH, false>(a, gain_wide, (int64_t)(blockIdx.x - columns) * kTeams + team, (int64_t)(gridDim.x - columns) * kTeams, t,
+                                      sums, at, none);
+    return;
+  }
+  const int p = threadIdx.x % kOncePieces, c = (int)(blockIdx.x * kOncePieces + p) * N, last = (int)a.cols - N;
+  const Piece at = {c < last ? c : last, 0, c < (int)a.cols};
+  float sum[N] = {};
+#pragma unroll 4
+  for (int64_t row = threadIdx.x / kOncePieces; row < a.rows; row += kRows) {
+    const Raw<T, N> d = load_piece<T>(row_of<T>(a.dy, row), at), h = load_piece<T>(row_of<T>(a.h, row), at);
+    const float inverse = a.inverse[row];
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[j] = fmaf(d.get(j), h.get(j) * inverse, sum[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+#pragma unroll
+    for (int m = kOncePieces; m < 64; m *= 2) sum[j] += __shfl_xor(sum[j], m);
+    if (threadIdx.x % 64 < kOncePieces) meet[threadIdx.x / 64][p][j] = sum[j];
+  }
+  __syncthreads();
+  if (threadIdx.x >= kOncePieces) return;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    for (int w = 1; w < kWaves; ++w) sum[j] += meet[w][p][j];
+  store_gain<T>(a, gain_wide, at, sum);
 }
 
 template <int T, int GT, bool BITS8>
@@ -586,9 +649,24 @@ hipError_t backward_as(const NormBackward& a, int64_t slabs, hipStream_t s) {
   });
 }
 
+constexpr int64_t kOnceRows = 1024, kOnceBytes = 4 << 20;
+static_assert(16 * 16384 * 4 <= kOnceBytes, "rows of one workgroup have no other way to the gain's gradient");
+bool once(const NormBackward& a, int type) {
+  return a.dgain && a.rows && a.rows <= kOnceRows && a.rows * a.cols * (type == EMB_TYPE_FP32 ? 4 : 2) <= kOnceBytes;
+}
+
 template <int T>
 hipError_t backward_rows_as(const NormBackward& a, bool gain_wide, int64_t slabs, hipStream_t s) {
   return by_pieces<T>(pieces_of(a.cols, T), [&]<int TEAM, int CH>() {
+    if (once(a, T)) {
+      const uint32_t columns = (uint32_t)ceil_div(pieces_of(a.cols, T), kOncePieces);
+      const uint32_t rows = (uint32_t)ceil_div(a.rows, kGroup<TEAM> / TEAM);
+      const bool over = a.dx.p == a.dy.p || a.dx.p == a.h.p;
+      if (over) k_norm_gradients_once<T, TEAM, CH><<<columns, kGroup<TEAM>, 0, s>>>(a, gain_wide, columns);
+      const uint32_t left = over ? 0 : columns;
+      k_norm_gradients_once<T, TEAM, CH><<<left + rows, kGroup<TEAM>, 0, s>>>(a, gain_wide, left);
+      return hipGetLastError();
+    }
     return in_launches(slabs, kGroup<TEAM>, [&](int64_t first, unsigned n) {
       k_norm_gradients<T, TEAM, CH><<<n, kGroup<TEAM>, 0, s>>>(a, gain_wide, first, slabs);
       return hipGetLastError();
@@ -602,8 +680,8 @@ hipError_t backward_rows_as(const NormBackward& a, bool gain_wide, int64_t slabs
 bool norm_in_registers(int64_t cols, int type) { return cols >= (type == EMB_TYPE_FP32 ? 4 : 8) && cols <= 16384; }
 
 // Workgroups that share the rows, each with a part of the gain's gradient: two to a CU, but no more than have two rows a
-// team, and none with more than kNormSlabRows a team.  Up to four rows a team are one workgroup's, which needs no join
-// (a launch of 3 us).
+// team, and none with more than kNormSlabRows a team.  One, which needs no part, for up to four rows a team: their gain's
+// gradient is always of the single launch.
 int64_t norm_slabs(int64_t rows, int64_t cols, int type) {
   if (!norm_in_registers(cols, type)) return ceil_div(rows, kNormSlabRows);
   const int64_t teams = pieces_of(cols, type) <= 256 ? 4 : 1;
@@ -638,7 +716,7 @@ hipError_t launch_norm_backward(const NormBackward& a, int type, bool gain_wide,
     else
       e = gain_wide ? backward_as<EMB_TYPE_FP16, EMB_TYPE_FP32>(a, slabs, s) : backward_as<EMB_TYPE_FP16, EMB_TYPE_FP16>(a, slabs, s);
   }
-  const bool joined = slabs == 1 && norm_in_registers(a.cols, type);
+  const bool joined = norm_in_registers(a.cols, type) && once(a, type);
   return e == hipSuccess && a.dgain && !joined ? join(a, slabs, gain_wide ? EMB_TYPE_FP32 : type, s) : e;
 }
 

@@ -123,6 +123,25 @@ def test_backward_over_many_rows(torch):
         assert torch.equal(dx, again[0]) and torch.equal(dgain, again[1])
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 17, 2048), ("fp16", 40, 8), ("fp32", 33, 16383), ("bf16", 257, 8160), ("fp32", 1024, 1024),
+                                             ("fp32", 1024, 1028), ("bf16", 1024, 29), ("bf16", 1025, 29), ("fp16", 1023, 2049)])
+def test_backward_of_few_rows(torch, dtype, rows, cols):
+    """Both sides of the rule by which both gradients go in one launch; results do not depend on where dx lies."""
+    from paper_2010_11305_amd import rmsnorm
+
+    x, _, gain, dy, dh = inputs(torch, rows, cols, dtype, 6, gain_dtype=dtype)
+    _, h, inverse = rmsnorm.norm_train(x, gain, eps=EPS)
+    dx, dgain = rmsnorm.backward(dy, h, inverse, gain.float(), dh=dh)
+    check_gradients(dx, dgain, dy, h, gain.float(), dh, dtype)
+    for over in range(3):
+        t = [v.clone() for v in (dy, h, dh)]
+        got = rmsnorm.backward(t[0], t[1], inverse, gain, dh=t[2], out=t[over])
+        assert torch.equal(got[0], dx) and torch.equal(got[1], dgain.to(gain.dtype))
+    wide = torch.full((rows, cols + 5), 7.0, dtype=x.dtype, device="cuda")
+    got = rmsnorm.backward(dy, h, inverse, gain, dh=dh, out=wide[:, 2:-3])
+    assert torch.equal(wide[:, 2:-3], dx) and (wide[:, :2] == 7).all() and (wide[:, -3:] == 7).all()
+
+
 def test_gradients_against_differences(torch):
     """Central differences of sum(w y) in 64 bits around FP32 inputs: steps of 2^-10 of values near 1 leave an error of
     their square, 2^-20, times third derivatives of a few units."""
