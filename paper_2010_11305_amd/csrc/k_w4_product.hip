@@ -415,7 +415,9 @@ __global__ __launch_bounds__(256) void k_w4_rows(W4Linear a, W4 w, Prepared out,
 template <int T>
 constexpr int kMostTiles = T == EMB_TYPE_FP32 ? 2 : 4;   // of 16 rows: an operand of FP32 rows takes three times the registers
 template <int RT>
-constexpr int kMoreWaves = RT == 2 ? 12 : 16;            // 168 registers a wave, or 128
+constexpr int kMoreWaves = RT == 4 ? 8 : RT == 2 ? 12 : 16;   // 256 registers a wave, 168 or 128
+
+constexpr int64_t kCus = 256;
 
 struct WavePairs {       // scales and biases of a wave's tile, in LDS
   uint16_t scales[64];   // of group g of the tile and row r of w at 16 g + r
@@ -539,8 +541,15 @@ hipError_t more_as(const W4Linear& a, const W4& w, const Prepared& in, hipStream
 
 template <int T, int G, int MT>
 hipError_t more_of(const W4Linear& a, const W4& w, const Prepared& in, hipStream_t s) {
-  // 32 outputs a workgroup, and x read half as often, where that still is a workgroup for every CU
-  return w.row_tiles * ceil_div(in.tiles, MT) >= 512 ? more_as<T, G, MT, 2>(a, w, in, s) : more_as<T, G, MT, 1>(a, w, in, s);
+  // A workgroup fills a CU.  Of 32 outputs, it reads x half as often; taken where that still is one for every CU.  Of 64, it
+  // takes four thirds of the time and halves the rounds of the CUs, to which an odd one counts in full: two rounds for
+  // three take as long.  64 BF16 rows of 4096, groups of 32 (and 128), 32 and 64 outputs a workgroup, us: to 8192 outputs 17.5 and
+  // 23.5 (15.9 and 18.4), 12800 27.3 and 23.7 (25.3 and 19.1), 20480 39.7 and 41.6 (36.3 and 33.2), 32768 53.7 and 43.8 (48.1 and 36.2);
+  // 32 rows to 12800 17.9 and 15.5 (17.1 and 13.9).  FP32 rows have no registers for it.
+  const int64_t blocks = ceil_div(in.tiles, MT), rounds2 = ceil_div(ceil_div(w.row_tiles, 2) * blocks, kCus);
+  if constexpr (MT >= 2 && T != EMB_TYPE_FP32)
+    if (3 * ceil_div(ceil_div(w.row_tiles, 4) * blocks, kCus) < 2 * rounds2) return more_as<T, G, MT, 4>(a, w, in, s);
+  return w.row_tiles * blocks >= 2 * kCus ? more_as<T, G, MT, 2>(a, w, in, s) : more_as<T, G, MT, 1>(a, w, in, s);
 }
 
 // Bytes of LDS that x takes in k_w4_few (of a block of 16 rows where there are more); as it is: of FP32 rows.
