@@ -541,15 +541,16 @@ hipError_t more_as(const W4Linear& a, const W4& w, const Prepared& in, hipStream
 
 template <int T, int G, int MT>
 hipError_t more_of(const W4Linear& a, const W4& w, const Prepared& in, hipStream_t s) {
-  // A workgroup fills a CU.  Of 32 outputs, it reads x half as often; taken where that still is one for every CU.  Of 64, it
-  // takes four thirds of the time and halves the rounds of the CUs, to which an odd one counts in full: two rounds for
-  // three take as long.  64 BF16 rows of 4096, groups of 32 (and 128), 32 and 64 outputs a workgroup, us: to 8192 outputs 17.5 and
-  // 23.5 (15.9 and 18.4), 12800 27.3 and 23.7 (25.3 and 19.1), 20480 39.7 and 41.6 (36.3 and 33.2), 32768 53.7 and 43.8 (48.1 and 36.2);
-  // 32 rows to 12800 17.9 and 15.5 (17.1 and 13.9).  FP32 rows have no registers for it.
+  // A workgroup fills a CU.  Of 32 outputs, it takes less than twice the time, as it reads x half as often: taken where there are more
+  // than CUs.  Of 64, it takes four thirds of that and halves the rounds of the CUs, to which an odd one counts in full: two
+  // rounds for three take as long.  64 BF16 rows of 4096, groups of 32 (and 128), us, with 16 and 32 outputs a workgroup: to 4096
+  // outputs 12.8 and 15.4 (12.0 and 14.3), 5120 18.9 and 15.5 (18.5 and 14.4); with 32 and 64: to 8192 17.5 and 23.5 (15.9 and 18.4),
+  // 12800 27.3 and 23.7 (25.3 and 19.1), 20480 39.7 and 41.6 (36.3 and 33.2), 32768 53.7 and 43.8 (48.1 and 36.2).  20 FP32 rows to
+  // 4352 with 16 and 32: 22.1 and 15.6 (21.4 and 15.3); they have no registers for 64.
   const int64_t blocks = ceil_div(in.tiles, MT), rounds2 = ceil_div(ceil_div(w.row_tiles, 2) * blocks, kCus);
   if constexpr (MT >= 2 && T != EMB_TYPE_FP32)
     if (3 * ceil_div(ceil_div(w.row_tiles, 4) * blocks, kCus) < 2 * rounds2) return more_as<T, G, MT, 4>(a, w, in, s);
-  return w.row_tiles * blocks >= 2 * kCus ? more_as<T, G, MT, 2>(a, w, in, s) : more_as<T, G, MT, 1>(a, w, in, s);
+  return w.row_tiles * blocks > kCus ? more_as<T, G, MT, 2>(a, w, in, s) : more_as<T, G, MT, 1>(a, w, in, s);
 }
 
 // Bytes of LDS that x takes in k_w4_few (of a block of 16 rows where there are more); as it is: of FP32 rows.

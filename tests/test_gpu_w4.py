@@ -330,7 +330,7 @@ def test_graph_and_streams(torch):
 
 # the largest rows that k_w4_few holds as operands (16 x 2048 in 16 bits) and as FP32 (16 x 2048), and those past them
 LARGE = [(16, 40, 2048), (16, 40, 2049), (5, 40, 6500), (16, 20, 4096), (16, 20, 4097), (16, 33, 8200), (16, 8200, 8200), (17, 4000, 2200), (20, 8200, 1200), (40, 3000, 2100), (48, 8177, 700), (64, 2100, 2100), (70, 8200, 520), (7, 50, 4100),
-         (200, 1700, 1000), (33, 8209, 1100), (64, 8257, 600), (128, 4193, 1300), (25, 17000, 900)]
+         (200, 1700, 1000), (33, 8209, 1100), (64, 8257, 600), (128, 4193, 1300), (25, 17000, 900), (24, 4113, 1300), (60, 5000, 400)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16", "int8"])
