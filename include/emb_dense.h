@@ -325,14 +325,16 @@ int emb_clip_destroy(emb_clip_t h);
 
 /* norm and factor into result[0] and result[1] (FP32 on the device).  grads: a host array of num_tensors device
  * pointers (read during the call only), each tensor contiguous, at any alignment of its type; NULL counts as zeros.
- * max_norm > 0, infinity for no limit.  workspace: 256-byte aligned.  Enqueue-only. */
+ * max_norm > 0, infinity for no limit.  workspace: 256-byte aligned.  Neither `result` nor the workspace may share
+ * memory with a gradient, with each other or with the handle's buffer.  Enqueue-only. */
 int emb_clip_norm(emb_clip_t h, const void* const* grads, double max_norm, float* result, void* workspace,
                   size_t workspace_bytes, void* stream);
 /* grads[t] = grads[t] * *factor, an FP32 product rounded to the tensor's type (nearest even); nothing is written where
- * *factor is 1.  No two tensors may share memory, nor hold `factor`.  NULL ones are left out.  Enqueue-only. */
+ * *factor is 1.  No two tensors may share memory, nor hold `factor` or lie over the handle's buffer.  NULL ones are
+ * left out.  Enqueue-only. */
 int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* stream);
-/* Both: norm and factor into `result`, and the gradients multiplied by the factor.  No two tensors may share memory, nor
- * hold `result`.  Enqueue-only. */
+/* Both: norm and factor into `result`, and the gradients multiplied by the factor, under the conditions of both.
+ * Enqueue-only. */
 int emb_clip_apply(emb_clip_t h, void* const* grads, double max_norm, float* result, void* workspace,
                    size_t workspace_bytes, void* stream);
 

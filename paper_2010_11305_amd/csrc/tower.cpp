@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 #include <utility>
 #include <vector>
@@ -73,12 +74,23 @@ bool w4_ok(int64_t rows, int64_t cols, int32_t group) {
   return (double)W4(nullptr, rows, cols, group).bytes() <= kMaxBytes;
 }
 
+// Bytes from begin to end; none of an absent buffer.
+struct Range {
+  uintptr_t begin = 0, end = 0;
+  bool meets(const Range& o) const { return begin < o.end && o.begin < end; }
+};
+Range range(const void* p, size_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return p && bytes ? Range{at, at + bytes} : Range{};
+}
+
 }  // namespace
 
 struct emb_clip {
   std::vector<int64_t> sizes, part0;   // part0[t]: first part of tensor t, part0[num_tensors] their number
   std::vector<int32_t> types;
   ClipDev dev;
+  Range state;
 };
 
 namespace {
@@ -143,30 +155,38 @@ bool grads_ok(const emb_clip* h, const void* const* grads) {
   return true;
 }
 
-// Whether no two gradients share memory, nor one with `other`.  Gradients mostly lie one behind the other already.
-bool apart(const emb_clip* h, const void* const* grads, const void* other, size_t bytes) {
-  const uintptr_t o = reinterpret_cast<uintptr_t>(other);
-  const auto place = [&](size_t t) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(grads[t]);
-    return std::pair<uintptr_t, uintptr_t>(at, at + (uintptr_t)h->sizes[t] * type_bytes(h->types[t]));
-  };
+Range place(const emb_clip* h, const void* const* grads, size_t t) { return range(grads[t], (size_t)h->sizes[t] * type_bytes(h->types[t])); }
+
+// Whether no gradient shares memory with one of `others`.
+bool clear_of(const emb_clip* h, const void* const* grads, std::initializer_list<Range> others) {
+  for (size_t t = 0; t < h->sizes.size(); ++t) {
+    const Range p = place(h, grads, t);
+    for (const Range& o : others)
+      if (p.meets(o)) return false;
+  }
+  return true;
+}
+
+// Whether no two gradients share memory.  They mostly lie one behind the other already.
+bool apart(const emb_clip* h, const void* const* grads) {
   uintptr_t end = 0;
   bool rising = true;
   size_t there = 0;
   for (size_t t = 0; t < h->sizes.size(); ++t) {
-    if (!h->sizes[t] || !grads[t]) continue;
-    const auto p = place(t);
-    if (p.first < o + bytes && o < p.second) return false;
-    rising = rising && p.first >= end;
-    end = p.second;
+    const Range p = place(h, grads, t);
+    if (!p.end) continue;
+    rising = rising && p.begin >= end;
+    end = p.end;
     ++there;
   }
   if (rising) return true;
   try {
     std::vector<std::pair<uintptr_t, uintptr_t>> places;
     places.reserve(there);
-    for (size_t t = 0; t < h->sizes.size(); ++t)
-      if (h->sizes[t] && grads[t]) places.push_back(place(t));
+    for (size_t t = 0; t < h->sizes.size(); ++t) {
+      const Range p = place(h, grads, t);
+      if (p.end) places.emplace_back(p.begin, p.end);
+    }
     std::sort(places.begin(), places.end());
     for (size_t i = 1; i < places.size(); ++i)
       if (places[i].first < places[i - 1].second) return false;
@@ -176,12 +196,15 @@ bool apart(const emb_clip* h, const void* const* grads, const void* other, size_
   }
 }
 
-// The checks of a call that takes a norm, and the parts' sums of squares into the workspace.
+// The checks of a call that takes a norm, and the parts' sums of squares into the workspace.  What is written (the parts'
+// sums, which are read until the last launch, and the result) lies over nothing that is read, nor over the tables.
 int squares(const emb_clip* h, const void* const* grads, double max_norm, float* result, void* workspace, size_t workspace_bytes,
             void* stream) {
   if (!h || !grads || !(max_norm > 0.0) || !result || reinterpret_cast<uintptr_t>(result) % 4 || !grads_ok(h, grads)) return EMB_EINVAL;
   const size_t need = clip_workspace(h->part0.back());
   if (need && (!workspace || !aligned(workspace))) return EMB_EINVAL;
+  const Range r = range(result, 8), w = range(workspace, need);
+  if (r.meets(w) || r.meets(h->state) || w.meets(h->state) || !clear_of(h, grads, {r, w})) return EMB_EINVAL;
   if (workspace_bytes < need) return EMB_ENOMEM;
   return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
     return launch_clip_squares(h->dev, ptr, first, part0, some, static_cast<double*>(workspace), S(stream));
@@ -353,6 +376,7 @@ int emb_clip_create(const emb_clip_config* cfg, void* state, size_t state_bytes,
     }
     h->part0 = p.part0;
     uint8_t* b = static_cast<uint8_t*>(state);
+    h->state = range(state, p.bytes);
     h->dev = {reinterpret_cast<const ClipTensor*>(b + p.o_tensors), reinterpret_cast<const AdamPart*>(b + p.o_parts)};
     hipError_t e = hipMemcpyAsync(b + p.o_tensors, p.tensors.data(), sizeof(ClipTensor) * p.tensors.size(), hipMemcpyHostToDevice, S(stream));
     if (e == hipSuccess && !parts.empty())
@@ -383,7 +407,9 @@ int emb_clip_norm(emb_clip_t h, const void* const* grads, double max_norm, float
 }
 
 int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* stream) {
-  if (!h || !grads || !factor || reinterpret_cast<uintptr_t>(factor) % 4 || !grads_ok(h, grads) || !apart(h, grads, factor, 4)) return EMB_EINVAL;
+  if (!h || !grads || !factor || reinterpret_cast<uintptr_t>(factor) % 4 || !grads_ok(h, grads) || !apart(h, grads) ||
+      !clear_of(h, grads, {range(factor, 4), h->state}))
+    return EMB_EINVAL;
   return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {
     return launch_clip_scale(h->dev, ptr, first, part0, some, factor, S(stream));
   }));
@@ -391,7 +417,7 @@ int emb_clip_scale(emb_clip_t h, void* const* grads, const float* factor, void* 
 
 int emb_clip_apply(emb_clip_t h, void* const* grads, double max_norm, float* result, void* workspace, size_t workspace_bytes,
                    void* stream) {
-  if (!h || !grads || !result || !grads_ok(h, grads) || !apart(h, grads, result, 8)) return EMB_EINVAL;
+  if (!h || !grads || !grads_ok(h, grads) || !apart(h, grads) || !clear_of(h, grads, {h->state})) return EMB_EINVAL;
   const int64_t parts = h->part0.back();
   if (!parts) return emb_clip_norm(h, grads, max_norm, result, workspace, workspace_bytes, stream);
   const int st = squares(h, grads, max_norm, result, workspace, workspace_bytes, stream);
