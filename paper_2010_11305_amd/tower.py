@@ -67,29 +67,29 @@ class Tower:
         """Logits of pooled rows [batch, width]."""
         if self.norm:
             return self._normed(x, lambda i, rows, past: self.rmsnorm.norm(rows, self.gains[i], residual=past),
-                                lambda i, rows: self.torch.relu_(self.layers[i].forward(rows).add_(self.biases[i])))
+                                lambda i, rows: self.torch.relu_(self.layers[i].forward(rows).add_(self.biases[i])), self.last)
         for layer, b in zip(self.layers, self.biases):
             x = self.torch.relu_(layer.forward(x).add_(b))
         return x @ self.last
 
-    def _normed(self, x, norm, layer):
-        """Logits by norm(i, rows, past) -> (normed rows, rows + past) and layer(i, normed rows) -> activations."""
+    def _normed(self, x, norm, layer, last):
+        """Logits by norm(i, rows, past) -> (normed rows, rows + past), layer(i, normed rows) -> activations, and the last layer."""
         past = None     # the rows that go around the layer before
         for i, adds in enumerate(self.adds):
             rows, x = norm(i, x, past)
             past, x = (x if adds else None), layer(i, rows)
-        return (x if past is None else x.add_(past)) @ self.last
+        return (x if past is None else x.add_(past)) @ last
 
     def serve(self, group=128):
-        """A function from pooled rows to logits as predict gives them, for serving a tower with `norm`: its weights now, in 4 bits
-        with a scale and a bias for each `group` columns, and rows in 8 bits."""
+        """A function from pooled rows to logits as predict gives them, for serving a tower with `norm`: its parameters now
+        (later changes do not reach it), weights in 4 bits with a scale and a bias for each `group` columns, and rows in 8 bits."""
         if not self.norm:
             raise ValueError("a tower without norms has no rows in 8 bits")
         rmsnorm, w4 = self.rmsnorm, self.w4
         weights = [w4.quantize(w, group) for w in self.weights]
-        gains, biases = [g.clone() for g in self.gains], [b.clone() for b in self.biases]
+        gains, biases, last = [g.clone() for g in self.gains], [b.clone() for b in self.biases], self.last.clone()
         return lambda x: self._normed(x, lambda i, rows, past: rmsnorm.norm8(rows, gains[i], residual=past),
-                                      lambda i, rows: w4.linear(rows, weights[i], bias=biases[i], relu=True, dtype=x.dtype))
+                                      lambda i, rows: w4.linear(rows, weights[i], bias=biases[i], relu=True, dtype=x.dtype), last)
 
     def gradients(self, x, labels, step):
         """(loss, gradients of the parameters, gradient of x)."""
