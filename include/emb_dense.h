@@ -239,8 +239,9 @@ int emb_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_
  *   dx = (dn - n * mean(dn * n)) * inverse + dsum   in `type`: the gradient of x and of the residual alike
  *   dgain = sum over the rows of dy * n             in gain_type
  * h and inverse are those of the forward pass; dsum [rows][cols] is what reaches h past the norm, or NULL.  dgain NULL
- * where it is not wanted.  Sums in FP32 over at most 256 rows and of at most four such, the rest in FP64, in an order that is a
- * function of the sizes.  dx may be dy, h or dsum itself; no other elements may be shared.
+ * where it is not wanted.  The mean's products and sum are of FP64 and do not overflow; dn, n and what follows the mean are
+ * FP32 operations.  The gain's sums are FP32 over at most 256 rows and of at most four such, the rest FP64.  The order of
+ * all sums is a function of the sizes.  dx may be dy, h or dsum itself; no other elements may be shared.
  * workspace: emb_rmsnorm_backward_workspace bytes, 256-byte aligned, or NULL when that is 0.  Enqueue-only. */
 int emb_rmsnorm_backward_workspace(int32_t type, int64_t rows, int64_t cols, size_t* bytes);
 int emb_rmsnorm_backward(const void* dy, int32_t type, int64_t rows, int64_t cols, int64_t lddy, const void* h, int64_t ldh,

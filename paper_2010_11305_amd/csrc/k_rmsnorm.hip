@@ -8,7 +8,9 @@
 // 7.6 to join 512 parts of the gain's; in passes over memory the same took 348 and 706.  4096 x 8192 to 8 bits, with a
 // residual, 47.7 us (4.9 TB/s), the codes to BF16 16.8 (6.0).  What little there is takes the launch and two or three trips to
 // memory: 2048 x 416 FP32 3.7, 5.2 and 2.5 us, one row of 12800 to 8 bits 4.7.
-// Squares are summed in FP64, which costs nothing there: no row of FP32 overflows or vanishes.
+// Squares are summed in FP64, which costs nothing there: no row of FP32 overflows or vanishes.  So is the mean that the
+// gradients subtract: with its sum in FP32, terms of 2^123 passed the type's end from 32 columns on, and 16384 x 12800 took 8 us
+// less of 331, 1000 x 1029 FP16 as long, 20000 x 64, where its shuffles count, 12.1 us instead of 13.6.
 #include "dense_device.h"
 
 namespace embd {
@@ -267,7 +269,7 @@ __device__ __forceinline__ void store_gain(const NormBackward& a, bool gain_wide
 
 // Rows first, first + step, .. in the registers of a team.  SUMS: their part of the gain's gradient goes to `sum`.
 template <int T, int TEAM, int CH, bool SUMS>
-__device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_wide, int64_t first, int64_t step, int t, float* sums,
+__device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_wide, int64_t first, int64_t step, int t, double* sums,
                                               Piece (&at)[CH], float (&sum)[SUMS ? CH : 1][kPiece<T>]) {
   constexpr int N = kPiece<T>;
   float g[CH][N];
@@ -279,7 +281,7 @@ __device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_w
 #pragma unroll
       for (int j = 0; j < N; ++j) sum[k][j] = 0.0f;
   }
-  const float cols = (float)a.cols;
+  const double cols = (double)a.cols;
   for (int64_t row = first; row < a.rows; row += step) {
     Raw<T, N> d[CH], h[CH], s[CH] = {};
 #pragma unroll
@@ -291,16 +293,16 @@ __device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_w
       for (int k = 0; k < CH; ++k) s[k] = load_piece<T>(row_of<T>(a.dsum, row), at[k]);
     }
     const float inverse = a.inverse[row];
-    float along = 0.0f;
+    double along = 0.0;
 #pragma unroll
     for (int k = 0; k < CH; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float u = h[k].get(j) * inverse, dj = d[k].get(j);
-        along = fmaf(k < CH / 2 || j >= at[k].skip ? dj * g[k][j] : 0.0f, u, along);
+        along = fma((double)(k < CH / 2 || j >= at[k].skip ? dj * g[k][j] : 0.0f), (double)u, along);
         if constexpr (SUMS) sum[k][j] = fmaf(dj, u, sum[k][j]);
       }
-    const float mean = block_sum<float, TEAM>(along, sums) / cols;
+    const float mean = (float)(block_sum<double, TEAM>(along, sums) / cols);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       Raw<T, N> out = {};
@@ -317,7 +319,7 @@ __device__ __forceinline__ void gradient_rows(const NormBackward& a, bool gain_w
 template <int T, int TEAM, int CH>
 __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a, bool gain_wide, int64_t first, int64_t blocks) {
   constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM;
-  __shared__ float sums[TEAM / 64];
+  __shared__ double sums[TEAM / 64];
   __shared__ float meet[kTeams > 1 ? kTeams - 1 : 1][kTeams > 1 ? CH * N * TEAM : 1];
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int64_t block = first + blockIdx.x;
@@ -362,7 +364,7 @@ constexpr int kOncePieces = 4;
 template <int T, int TEAM, int CH>
 __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients_once(NormBackward a, bool gain_wide, uint32_t columns) {
   constexpr int N = kPiece<T>, kTeams = kGroup<TEAM> / TEAM, kRows = kGroup<TEAM> / kOncePieces, kWaves = kGroup<TEAM> / 64;
-  __shared__ float sums[TEAM / 64];
+  __shared__ double sums[TEAM / 64];
   __shared__ float meet[kWaves][kOncePieces][N];
   if (blockIdx.x >= columns) {
     const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_dx(NormBackward a, int64_t fi
     part(c, n, dn, u);
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-      if (j < n) along += (double)(dn[j] * u[j]);
+      if (j < n) along = fma((double)dn[j], (double)u[j], along);
   }
   const float mean = (float)(block_sum<double, kThreads>(along, sums) / (double)a.cols);
   for (int64_t c = (int64_t)threadIdx.x * kPer; c < a.cols; c += kThreads * kPer) {
