@@ -96,13 +96,15 @@ def _forward(x, gain, residual, eps, out, sum_out, inverse):
 
 def norm(x, gain=None, residual=None, eps=1e-6, out=None, sum_out=None):
     """(y, h) for rows x [rows, cols]: h = x + residual (x itself without one), y = h / sqrt(mean(h^2) + eps) * gain.
-    out and sum_out may be x or the residual, to work in place."""
+    out and sum_out may be x or the residual, to work in place (without a residual, out over x leaves no h)."""
     return _forward(x, gain, residual, eps, out, sum_out, False)[:2]
 
 
 def norm_train(x, gain=None, residual=None, eps=1e-6, out=None, sum_out=None):
     """(y, h, inverse): norm, with the rows' 1 / sqrt(mean(h^2) + eps) that backward takes.  h must keep its values until
-    then."""
+    then: without a residual it is x, and out must lie elsewhere."""
+    if residual is None and out is not None and out.data_ptr() == x.data_ptr() and x.numel():
+        raise ValueError("out lies over x, which is the h that the backward pass takes")
     return _forward(x, gain, residual, eps, out, sum_out, True)
 
 
