@@ -133,8 +133,10 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipDev d, ClipPoin
   scale(d, ptr, first, part0 + blockIdx.x, *factor);
 }
 
-// The join and the scaling at once: every workgroup adds up the parts for itself (some 2000 values from the L2, while a
-// launch of one workgroup and the gap behind it take 4 us).
+// The join and the scaling at once: every workgroup adds up all parts for itself, from the L2.  For the tensors of one launch, which
+// have 2048 parts and one a tensor at most; every launch more would add them up again, in each of its workgroups.  us in a
+// graph, both kernels, against a join of one workgroup and k_clip_scale: 6 tensors of 58,000 4.4 (5.6), 480 of 1000 6.9 (7.6),
+// 480 of 8192 15.4 (16.1); of several launches 1000 of 1000 20.6 (19.1), 4000 73 (62), 30,000 of 100 822 (378).
 __global__ __launch_bounds__(kClipThreads) void k_clip_join_scale(ClipDev d, ClipPointers ptr, uint32_t first, int64_t part0,
                                                                   const double* __restrict__ partial, int64_t parts,
                                                                   double max_norm, float* __restrict__ result) {

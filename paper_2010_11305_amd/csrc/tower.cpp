@@ -420,6 +420,10 @@ int emb_clip_apply(emb_clip_t h, void* const* grads, double max_norm, float* res
   if (!h || !grads || !grads_ok(h, grads) || !apart(h, grads) || !clear_of(h, grads, {h->state})) return EMB_EINVAL;
   const int64_t parts = h->part0.back();
   if (!parts) return emb_clip_norm(h, grads, max_norm, result, workspace, workspace_bytes, stream);
+  if (h->sizes.size() > (size_t)kClipTensors) {   // of more than one launch: joined once (k_clip_join_scale)
+    const int st = emb_clip_norm(h, grads, max_norm, result, workspace, workspace_bytes, stream);
+    return st != EMB_OK ? st : emb_clip_scale(h, grads, result + 1, stream);
+  }
   const int st = squares(h, grads, max_norm, result, workspace, workspace_bytes, stream);
   if (st != EMB_OK) return st;
   return status(over_tensors(h, grads, [&](const ClipPointers& ptr, uint32_t first, int64_t part0, unsigned some) {

@@ -95,3 +95,13 @@ def test_nothing_to_read():
     assert c.norm([A, A], A, None) == (0, ["join"]) and c.apply([None, A], A, A) == (0, ["join"])
     assert c.scale([A, A], A) == (0, [])
     assert c.norm([A, A], c.state, None) == (ec.EMB_EINVAL, [])
+
+
+def test_many_tensors_are_joined_once():
+    """Every workgroup of a launch that joins and scales adds up all parts, so that is left to what one launch carries: with a launch
+    for each 480 tensors the work would grow with their square."""
+    for n, want in ((1, ["squares", "join_scale"]), (480, ["squares", "join_scale"]), (481, 2 * ["squares"] + ["join"] + 2 * ["scale"]),
+                    (20000, 42 * ["squares"] + ["join"] + 42 * ["scale"])):
+        c = Clip([3] * n)
+        assert c.apply([A + 16 * k for k in range(n)], R, W) == (0, want)
+        assert c.apply([A] * n, R, W) == ((0, want) if n == 1 else (ec.EMB_EINVAL, []))
