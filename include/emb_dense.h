@@ -271,7 +271,8 @@ int emb_w4_dequantize(const void* q, int64_t rows, int64_t cols, int32_t group, 
                       void* stream);
 /* Between a W4 matrix and the plain form: codes [rows][ceil(cols / 2)], two a byte, the even column in the low half;
  * scales and biases FP16 [rows][ceil(cols / group)]; on the device and without padding.  With an odd number of
- * columns the last half byte of a row is ignored by pack and 0 from unpack.  Enqueue-only, as the two above. */
+ * columns the last half byte of a row is ignored by pack and 0 from unpack.  What is written shares no memory with anything
+ * else of a call, here and in the two above.  All enqueue-only. */
 int emb_w4_pack(const uint8_t* codes, const void* scales, const void* biases, int64_t rows, int64_t cols, int32_t group,
                 void* q, void* stream);
 int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint8_t* codes, void* scales, void* biases,

@@ -84,6 +84,18 @@ Range range(const void* p, size_t bytes) {
   return p && bytes ? Range{at, at + bytes} : Range{};
 }
 
+// A W4 matrix and its plain form.
+struct Plain {
+  Range q, codes, scales, biases;
+  Plain(const W4& w, const void* c, const void* s, const void* b)
+      : q(range(w.base, (size_t)w.bytes())),
+        codes(range(c, (size_t)(w.rows * ((w.cols + 1) / 2)))),
+        scales(range(s, (size_t)(w.rows * ceil_div(w.cols, w.group) * 2))),
+        biases(range(b, (size_t)(w.rows * ceil_div(w.cols, w.group) * 2))) {}
+  bool over_matrix() const { return q.meets(codes) || q.meets(scales) || q.meets(biases); }
+  bool over_each_other() const { return codes.meets(scales) || codes.meets(biases) || scales.meets(biases); }
+};
+
 }  // namespace
 
 struct emb_clip {
@@ -301,7 +313,9 @@ int emb_w4_pack(const uint8_t* codes, const void* scales, const void* biases, in
   if (rows == 0 || cols == 0) return EMB_OK;
   if (!codes || !scales || !biases || !q || !aligned(q)) return EMB_EINVAL;
   if (reinterpret_cast<uintptr_t>(scales) % 2 || reinterpret_cast<uintptr_t>(biases) % 2) return EMB_EINVAL;
-  return status(launch_w4_pack(codes, static_cast<const uint16_t*>(scales), static_cast<const uint16_t*>(biases), W4(q, rows, cols, group), S(stream)));
+  const W4 w(q, rows, cols, group);
+  if (Plain(w, codes, scales, biases).over_matrix()) return EMB_EINVAL;
+  return status(launch_w4_pack(codes, static_cast<const uint16_t*>(scales), static_cast<const uint16_t*>(biases), w, S(stream)));
 }
 
 int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint8_t* codes, void* scales, void* biases, void* stream) {
@@ -309,7 +323,10 @@ int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint
   if (rows == 0 || cols == 0) return EMB_OK;
   if (!codes || !scales || !biases || !q || !aligned(q)) return EMB_EINVAL;
   if (reinterpret_cast<uintptr_t>(scales) % 2 || reinterpret_cast<uintptr_t>(biases) % 2) return EMB_EINVAL;
-  return status(launch_w4_unpack(W4(q, rows, cols, group), codes, static_cast<uint16_t*>(scales), static_cast<uint16_t*>(biases), S(stream)));
+  const W4 w(q, rows, cols, group);
+  const Plain p(w, codes, scales, biases);
+  if (p.over_matrix() || p.over_each_other()) return EMB_EINVAL;
+  return status(launch_w4_unpack(w, codes, static_cast<uint16_t*>(scales), static_cast<uint16_t*>(biases), S(stream)));
 }
 
 int emb_w4_linear_workspace(int32_t type, int64_t m, int64_t n, int64_t k, int32_t group, size_t* bytes) {
