@@ -23,7 +23,8 @@ dtype_of = attrgetter("dtype")
 
 class GradClip:
     """params: tensors on one GPU whose gradients have their sizes and types (or all the type grad_dtype); any mixture of
-    float32, bfloat16 and float16.  max_norm: the largest norm, above 0 (infinity for none)."""
+    float32, bfloat16 and float16.  max_norm: the largest norm, above 0 (infinity for none).  Graphs that captured its calls
+    need it as long as they are replayed."""
 
     def __init__(self, params, max_norm: float = 1.0, grad_dtype=None):
         params = list(params)
@@ -43,8 +44,9 @@ class GradClip:
         self._state = torch.empty(max(s.state_bytes, 256), dtype=torch.uint8, device=self.device)
         self._h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            lib.check(L.emb_clip_create(ctypes.byref(c), self._state.data_ptr(), s.state_bytes,
-                                        torch.cuda.current_stream().cuda_stream, ctypes.byref(self._h)), "emb_clip_create")
+            self._stream = torch.cuda.current_stream().cuda_stream
+            lib.check(L.emb_clip_create(ctypes.byref(c), self._state.data_ptr(), s.state_bytes, self._stream, ctypes.byref(self._h)),
+                      "emb_clip_create")
 
     def close(self):
         if getattr(self, "_h", None):
@@ -68,6 +70,8 @@ class GradClip:
         if (list(map(Tensor.numel, given)) != sizes or not all(map(Tensor.is_contiguous, given))
                 or list(map(dtype_of, given)) != dtypes or not set(map(Tensor.get_device, given)) <= {self.device.index}):
             raise ValueError(f"gradients must be contiguous, on {self.device}, and each of the size and type of its parameter")
+        if torch._C._cuda_getCurrentRawStream(self.device.index) != self._stream:
+            self._state.record_stream(torch.cuda.current_stream(self.device))   # else the tables were anyone's once self is dropped
         return given, array("Q", map(Tensor.data_ptr, grads) if given is grads else [0 if g is None else g.data_ptr() for g in grads])
 
     def norm(self, grads):
