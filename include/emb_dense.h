@@ -241,7 +241,8 @@ int emb_rows8_dequantize(const int8_t* codes, int64_t rows, int64_t cols, int64_
  * h and inverse are those of the forward pass; dsum [rows][cols] is what reaches h past the norm, or NULL.  dgain NULL
  * where it is not wanted.  The mean's products and sum are of FP64 and do not overflow; dn, n and what follows the mean are
  * FP32 operations.  The gain's sums are FP32 over at most 256 rows and of at most four such, the rest FP64.  The order of
- * all sums is a function of the sizes.  dx may be dy, h or dsum itself; no other elements may be shared.
+ * all sums is a function of the sizes.  dx may be dy, h or dsum itself; no other elements may be shared.  (Up to 1024 rows
+ * and 4 MB, dx over dy or h takes another launch.)
  * workspace: emb_rmsnorm_backward_workspace bytes, 256-byte aligned, or NULL when that is 0.  Enqueue-only. */
 int emb_rmsnorm_backward_workspace(int32_t type, int64_t rows, int64_t cols, size_t* bytes);
 int emb_rmsnorm_backward(const void* dy, int32_t type, int64_t rows, int64_t cols, int64_t lddy, const void* h, int64_t ldh,
@@ -279,7 +280,8 @@ int emb_w4_unpack(const void* q, int64_t rows, int64_t cols, int32_t group, uint
                   void* stream);
 
 /* y [m][n] = x w^T + bias for rows x [m][k] and a W4 weight w [n][k], then max(y, 0) if `relu` (NaN stays NaN).  Made
- * for few rows (a weight is read once for each 64 of them); right for any number.
+ * for few rows: the weight is read once for each 64 of them at most (32 of FP32 rows; 16 where it is small); right for any
+ * number.
  *   type      of x: a full-precision type, or EMB_TYPE_INT8 with `scales` [m], the rows' scales (NULL otherwise)
  *   bias      [n] FP32, or NULL
  *   y_type    a full-precision type

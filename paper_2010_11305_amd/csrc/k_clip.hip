@@ -4,8 +4,9 @@
 // arguments.  Sums are kept in FP64: no FP32 gradient's square overflows or vanishes there, and its operations are as
 // fast as those of FP32.
 //
-// Memory bounds both kernels where there is much: 200M BF16 in 300 tensors, squares 86 us (4.7 TB/s), scaling 157 us
-// (5.1 TB/s); 350,000 FP32 in 6 tensors 3.2 and 3.8 us, of which a launch is most.
+// Memory bounds both kernels where there is much: by the kernel trace, 200M BF16 in 300 tensors, squares 83 us (4.8 TB/s; 120 right
+// behind a kernel that wrote them), join and scaling 156 (5.1 TB/s); 350,000 FP32 in 6 tensors 3.5 and 3.9 us, of which a launch
+// is most.
 #include "dense_device.h"
 
 namespace embd {

@@ -4,10 +4,12 @@
 // writes every value once; wider ones take a workgroup a row that goes over it as often as it has to, a thread
 // always over the same 8 columns at a time, so that what it wrote in one pass it reads in the next.
 //
-// Memory bounds them.  16384 x 12800 BF16 with a residual (1.68 GB each way): forward 277 us (6.1 TB/s), gradients 324 (5.2) and
-// 7.6 to join 512 parts of the gain's; in passes over memory the same took 348 and 706.  4096 x 8192 to 8 bits, with a
-// residual, 47.7 us (4.9 TB/s), the codes to BF16 16.8 (6.0).  What little there is takes the launch and two or three trips to
-// memory: 2048 x 416 FP32 3.7, 5.2 and 2.5 us, one row of 12800 to 8 bits 4.7.
+// Memory bounds them.  By the kernel trace, 16384 x 12800 BF16 with a residual (1.68 GB each way): forward 276 us (6.1 TB/s),
+// gradients 330 (5.1) and 7.6 to join 512 parts of the gain's.  4096 x 8192 to 8 bits, with a residual, 47.4 us (5.0 TB/s), the codes
+// to BF16 16.8 (6.0).  What little there is takes the launch and two or three trips to memory: 2048 x 416 FP32 3.7, 5.5 and
+// 2.7 us, one row of 12800 to 8 bits 4.7.  Rows that no registers hold are read two or three times: us a call with a residual in a graph,
+// forward and gradients, 8192 x 25600 BF16 409 (4.1 TB/s) and 716 (2.3), 8192 x 16384, in registers, 191 (5.6) and 217 (5.0).  Rows of less
+// than a piece take a workgroup each all the same: 2,000,000 x 3 2.7 ms.
 // Squares are summed in FP64, which costs nothing there: no row of FP32 overflows or vanishes.  So is the mean that the
 // gradients subtract: with its sum in FP32, terms of 2^123 passed the type's end from 32 columns on, and 16384 x 12800 took 8 us
 // less of 331, 1000 x 1029 FP16 as long, 20000 x 64, where its shuffles count, 12.1 us instead of 13.6.
@@ -356,10 +358,11 @@ __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients(NormBackward a,
 
 // Both gradients of few rows in one launch, without parts that a second one joins: the first `columns` workgroups each sum
 // four pieces of the gain's gradient over all rows, the others take the rows.  dy and h are read twice, the second time
-// from a cache.  Measured against k_norm_gradients and k_norm_gain_join, us in a graph: 256 x 416 in FP32 2.8 (5.4),
-// 256 x 8192 in BF16 4.7 (11.3), 1000 x 2048 in BF16 6.8 (9.4), 1000 x 1029 in FP32 8.1 (10.2); not taken beyond kOnceRows
-// and kOnceBytes: 2048 x 416 in FP32 8.6 (6.1), 1000 x 2048 in FP32 11.2 (11.1).  A dx that lies over dy or h waits for
-// the columns: two launches of the same kernel, with the same results (256 x 416 5.6, 1000 x 2048 in BF16 14.1).
+// from a cache.  Measured against k_norm_gradients and k_norm_gain_join, us in a graph: 256 x 416 in FP32 3.1 (5.9),
+// 256 x 8192 in BF16 5.0 (11.4), 1000 x 2048 in BF16 6.7 (9.9), 1000 x 1029 in FP16 7.1 (9.9); not taken beyond kOnceRows
+// and kOnceBytes: 2048 x 416 in FP32 8.2 (6.8), 4000 x 512 in BF16 12.1 (9.5), 1000 x 2048 in FP32 11.1 (11.2).  A dx that lies
+// over dy or h waits for the columns: two launches of the same kernel, so that the gain's gradient has the same bits wherever dx
+// lies.  That costs more than both: 256 x 416 5.9, 256 x 8192 11.0, 1000 x 1029 in FP16 13.1, 1000 x 2048 in BF16 14.5.
 constexpr int kOncePieces = 4;
 template <int T, int TEAM, int CH>
 __global__ __launch_bounds__(kGroup<TEAM>) void k_norm_gradients_once(NormBackward a, bool gain_wide, uint32_t columns) {

@@ -5,14 +5,17 @@
 // the same instruction with ones in their place, in the registers where the sums of products lie.  FP32 rows go
 // in as three BF16 parts that add up to them exactly.
 //
-// Few rows (k_w4_few) are bound by memory and by what every launch costs: 1 row, 4096 x 12800, groups of 128, 7.5 us a
-// call for 27.9 MB (3.7 TB/s), of which 3.3 us are left without the loop over the columns; 8-bit rows against 8192 x 8192
-// 8.2 us for 35.7 MB (4.4 TB/s).  Code runs once or twice in such a call, and its way from memory counts as much as the data's: with the
-// loop unrolled over 7 tiles, whose loads were all under way at once, the same took 10.5 and 12.7 us.  So loops stay short,
-// and what is rare goes value by value.
-// Up to 64 rows (k_w4_more): 64 rows, 8192 x 12800, 31.5 us with groups of 32 and 29 with groups of 128 (430 and 460 TFLOP/s), k_w4_rows'
-// 4 among them.  200 vector operations a wave and tile (128 of them scale sums), 40 matrix instructions and 420 MB of x out of the L2
-// take about as long each: without the loads of x 28 and 21 us, without those of w 27 and 25, without matrix instructions 32 and 20.
+// Few rows (k_w4_few) are bound by memory and by what every launch costs.  us a call in a graph, and of the kernel by its trace: 1 row,
+// 4096 x 12800, groups of 128 8.0 and 8.4 (27.9 MB, 3.5 TB/s), of which 3.3 are left without the loop over the columns; one 8-bit row
+// against 8192 x 8192 8.4 and 8.5 (35.7 MB, 4.2 TB/s).  Code runs once or twice in such a call, and its way from memory counts as
+// much as the data's: with the loop unrolled over 7 tiles, whose loads were all under way at once, the same took 3.0 and 4.5 us
+// more.  So loops stay short, and what is rare goes value by value.
+// Up to 64 rows (k_w4_more): 64 rows, 8192 x 12800, 31.7 us a call in a graph with groups of 32 and 29.1 with groups of 128 (423 and 461
+// TFLOP/s); by the trace 28.3 for groups of 32, and 5.0 for k_w4_rows.  No one thing bounds it: of the 57 thousand clocks of its waves
+// (24 us) the matrix pipe is busy for 34%, by the counters, vector instructions other than its own issue for 40% (groups of 128:
+// 25 and 31%), with three waves a SIMD that do not cover for each other: each waits for data 37% of its time and for its turn
+// at a pipe 40%.  Reads out of the L2 are 515 MB, 420 of them x; conflicts of LDS banks are 5 thousand clocks.  Without the loads of x it took 28 us (groups of 128: 21), without those of w 27 (25), without matrix
+// instructions 32 (20).
 #include "dense_device.h"
 
 namespace embd {
